@@ -498,6 +498,36 @@ int mpt_lstm_get_scale(mpt_lstm_ctx *ctx, float *S_out);
 const char *mpt_lstm_last_error(mpt_lstm_ctx *ctx);
 void mpt_lstm_destroy(mpt_lstm_ctx *ctx);
 
+/* ------------------------------------------------------------ layer normalisation
+ *
+ * Normalisation of each row over its features with a learned scale and shift (section 3.3 keeps the point-wise
+ * and reduction work of normalisation layers in FP32 on FP16 data; the paper's own are batch
+ * normalisations).  With n = cols, every sum and statistic in FP32:
+ *   mean = sum_c x[r,c] / n ;  rstd = 1 / sqrt(sum_c (x[r,c] - mean)^2 / n + eps)
+ *   y[r,c] = rn16((x[r,c] - mean) * rstd * gamma[c] + beta[c])
+ * and backward, with h = (x - mean) * rstd from the statistics passed in, g = dy * gamma:
+ *   dx     = rn16(rstd * (g - sum_c g / n - h * sum_c (g * h) / n))
+ *   dgamma = rn16(sum_r dy * h) ;  dbeta = rn16(sum_r dy)
+ * x, y, dy, dx: FP16 [rows, cols] with row pitches in elements.  gamma16 / beta16: FP16 [cols] (working
+ * copies, as the LSTM's bias); beta16 may be null (no shift) and dbeta16 may be null (not wanted).
+ * mean / rstd: float [rows]; the forward pass writes them for the backward pass, either may be null there.
+ * nonfinite_flag (may be null): a uint32 that is OR-ed with 1 when an element of dgamma or dbeta is inf or NaN
+ * (section 3.2).  Gradients are scaled by S if dy is; they are overwritten, not accumulated into.
+ * workspace: mpt_layernorm_workspace_bytes, 16-byte aligned, owned by the caller and in use until the call's
+ * stream work has completed (calls that may overlap need one each).  Results are run-to-run identical.
+ * Rows that are 16-byte aligned (base pointers, and pitches that are multiples of 8) move in 16-byte pieces, others
+ * element by element; any cols from 1 on is accepted.  Outputs must not overlap inputs (the same pointer is
+ * refused).  rows == 0: forward does nothing, backward writes zero dgamma and dbeta.  The stream must belong to
+ * the current device (the launch fails otherwise: MPT_ERR_CUDA).  Bytes moved per element: 4 forward, 6 backward. */
+int mpt_layernorm_forward(int rows, int cols, const uint16_t *x_dev, int ldx, const uint16_t *gamma16_dev,
+                          const uint16_t *beta16_dev, float eps, uint16_t *y_dev, int ldy, float *mean_dev, float *rstd_dev,
+                          void *cuda_stream);
+int mpt_layernorm_workspace_bytes(int rows, int cols, size_t *bytes_out);
+int mpt_layernorm_backward(int rows, int cols, const uint16_t *dy_dev, int lddy, const uint16_t *x_dev, int ldx,
+                           const uint16_t *gamma16_dev, const float *mean_dev, const float *rstd_dev, uint16_t *dx_dev, int lddx,
+                           uint16_t *dgamma16_dev, uint16_t *dbeta16_dev, uint32_t *nonfinite_flag_dev, void *workspace_dev,
+                           size_t workspace_bytes, void *cuda_stream);
+
 /* Softmax cross-entropy forward and scaled backward (sections 3.2, 3.3), arithmetic
  * as in mpt_backward_scaled.  z_dev/dz_dev: FP16 [B, C] with pitches ldz/lddz
  * (the two must not overlap).  row_loss_dev: float [B] scratch; loss_dev: one float,

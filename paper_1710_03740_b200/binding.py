@@ -39,6 +39,7 @@ EXPORTS = ["mpt_workspace_bytes", "mpt_create", "mpt_workspace_bytes_opt", "mpt_
            "mpt_lstm_set_dynamic_scale", "mpt_lstm_get_scale", "mpt_lstm_last_error", "mpt_lstm_destroy",
            "mpt_lstm_forward", "mpt_lstm_backward", "mpt_lstm_cell_forward", "mpt_lstm_cell_backward", "mpt_bias_grad",
            "mpt_add_f16",
+           "mpt_layernorm_forward", "mpt_layernorm_workspace_bytes", "mpt_layernorm_backward",
            "mpt_dp_shard", "mpt_dp_step_flat", "mpt_dp_alloc", "mpt_dp_free", "mpt_dp_export", "mpt_dp_open", "mpt_dp_close",
            "mpt_dp_layout_of", "mpt_dp_attach", "mpt_dp_step_flat_opt", "mpt_dp_norm_flat", "mpt_dp_norm",
            "mpt_workspace_bytes_dp", "mpt_create_dp", "mpt_state_range", "mpt_dp_overlap_events", "mpt_dp_overlap_attach",
@@ -156,6 +157,9 @@ def lib() -> C.CDLL:
     L.mpt_lstm_cell_backward.argtypes = [i32, i32, vp, i32, vp, i32, vp, i32, vp, i32, vp, i32, vp, i32, vp, i32, vp]
     L.mpt_bias_grad.argtypes = [vp, sz, i32, i32, vp, vp, vp, vp]
     L.mpt_add_f16.argtypes = [vp, i32, vp, i32, vp, i32, i32, i32, vp]
+    L.mpt_layernorm_forward.argtypes = [i32, i32, vp, i32, vp, vp, f32, vp, i32, vp, vp, vp]
+    L.mpt_layernorm_workspace_bytes.argtypes = [i32, i32, C.POINTER(sz)]
+    L.mpt_layernorm_backward.argtypes = [i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
     L.mpt_dp_shard.argtypes = [sz, i32, i32, C.POINTER(sz), C.POINTER(sz)]
     L.mpt_dp_step_flat.argtypes = [vp, vp, vp, vp, vp, sz, i32, i32, f32, f32, f32, vp, vp]
     L.mpt_dp_step_flat_opt.argtypes = [C.POINTER(Optimizer), vp, vp, vp, vp, vp, vp, sz, i32, i32, f32, f32, f32, vp, vp, vp, vp]
@@ -534,6 +538,46 @@ def mpt_bias_grad(dG, rows, cols, ld, parts, db16, nonfinite_flag=None, stream=N
 
 def mpt_add_f16(a, lda, b, ldb, out, ldo, rows, cols, stream=None):
     _check(lib().mpt_add_f16(_dptr(a), lda, _dptr(b), ldb, _dptr(out), ldo, rows, cols, _stream_ptr(stream)))
+
+
+# ------------------------------------------------------------ layer normalisation
+
+def _stream_of(stream, sizes):
+    """Raw handle of `stream` (default: the current one) after a look at the tensors of a call: `sizes` lists
+    (tensor or None, bytes per element).  All have to be on the current device; pointers of another one
+    would reach the kernels unseen."""
+    import torch
+    s = torch.cuda.current_stream() if stream is None else stream
+    at = s.device_index
+    for t, width in sizes:
+        if t is not None and (not t.is_cuda or t.get_device() != at or t.element_size() != width):
+            raise ValueError("expected a CUDA tensor of %d-byte elements on the stream's device (cuda:%d), got %s on %s"
+                             % (width, at, t.dtype, t.device))
+    return s.cuda_stream
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def mpt_layernorm_forward(rows, cols, x, ldx, gamma16, beta16, eps, y, ldy, mean=None, rstd=None, stream=None):
+    st = _stream_of(stream, ((x, 2), (gamma16, 2), (beta16, 2), (y, 2), (mean, 4), (rstd, 4)))
+    _check(lib().mpt_layernorm_forward(rows, cols, _at(x), ldx, _at(gamma16), _at(beta16), eps, _at(y), ldy, _at(mean), _at(rstd), st))
+
+
+def mpt_layernorm_workspace_bytes(rows, cols) -> int:
+    out = C.c_size_t(0)
+    _check(lib().mpt_layernorm_workspace_bytes(rows, cols, C.byref(out)))
+    return int(out.value)
+
+
+def mpt_layernorm_backward(rows, cols, dy, lddy, x, ldx, gamma16, mean, rstd, dx, lddx, dgamma16, dbeta16, workspace,
+                           nonfinite_flag=None, stream=None):
+    """workspace: a uint8 tensor of at least mpt_layernorm_workspace_bytes(rows, cols)."""
+    st = _stream_of(stream, ((dy, 2), (x, 2), (gamma16, 2), (mean, 4), (rstd, 4), (dx, 2), (dgamma16, 2), (dbeta16, 2),
+                             (nonfinite_flag, 4), (workspace, 1)))
+    _check(lib().mpt_layernorm_backward(rows, cols, _at(dy), lddy, _at(x), ldx, _at(gamma16), _at(mean), _at(rstd), _at(dx), lddx,
+                                        _at(dgamma16), _at(dbeta16), _at(nonfinite_flag), _at(workspace), workspace.numel(), st))
 
 
 class LstmLayer:
