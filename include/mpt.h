@@ -539,6 +539,37 @@ int mpt_softmax_ce(const uint16_t *z_dev, int ldz, const int32_t *labels_dev, in
                    uint16_t *dz_dev, int lddz, float *row_loss_dev, float *loss_dev,
                    uint32_t *bad_labels_dev, uint32_t *status_dev, void *cuda_stream);
 
+/* Linear layer over a large vocabulary and the softmax cross-entropy of its outputs in one call, without a logits
+ * matrix (sections 3.2, 3.3; the paper's language model, section 4.5, has 793K words and samples them instead).
+ *   z[i,v]  = sum_k x[i,k] * W[v,k]                          FP32, never stored or rounded
+ *   loss_i  = log sum_v exp(z[i,v]) - z[i,y_i]               row_loss_dev[i]; loss_dev = mean over the N rows
+ *   d[i,v]  = softmax(z_i)[v] - [v = y_i]
+ *   dx[i,:] = rn16(S/N * sum_v d[i,v] * W[v,:])              FP32 sums, S/N applied before the rounding
+ *   dW[v,:] = rn16(S/N * sum_i d[i,v] * x[i,:])
+ * The two gradients' products take d as FP16 scaled by 2^14 (rounded twice, each time by at most 2^-11 of the
+ * value down to d = 2^-28, and kept down to 2^-38), so no d is lost to a small S/N.
+ * x: FP16 [N, H], W: FP16 [V, H], dx like x, dW like W, row-major with pitches in elements; labels: int32 [N]
+ * on the device.  A label outside [0, V) contributes neither loss nor gradient, whatever its row of x holds (its
+ * row of dx is zero; the mean still divides by N).  dx_dev and dW_dev may each be null (not wanted; with both null only the losses are computed
+ * and S is ignored).  Gradients are overwritten, not accumulated into.  N == 0: loss 0, dW zero.
+ * bad_labels_dev (may be null): receives the number of labels outside [0, V).  nonfinite_flag_dev (may be null):
+ * OR-ed with 1 if any dW is inf or NaN (section 3.2).  status_dev (may be null): one uint32 the caller has zeroed,
+ * receives a time-out code if a bounded wait of a product kernel runs out (results are then invalid).
+ * H must be a multiple of 8, the four matrices 16-byte aligned with pitches that are multiples of 8
+ * (MPT_ERR_SHAPE otherwise; V and N are arbitrary, V at most MPT_LINEAR_CE_MAX_V).  Outputs must not overlap inputs.
+ * workspace: 256-byte aligned, mpt_linear_ce_workspace_bytes of the same N, V, H, row_block (want_dx, want_dW: whether
+ * dx_dev, dW_dev will be given), owned by the caller and in use until the call's stream work has completed: calls
+ * that may overlap, captured graphs among them, need one each.  The rows are worked on row_block at a time (a
+ * multiple of 256; 0: the library's choice of 4096), which bounds the workspace: about 2 * row_block * V bytes of FP16
+ * exponentials and 2 * row_block * H of x, and with more than one block 4 * V * H bytes in which dW is summed in FP32.
+ * Results are run-to-run identical.  Asynchronous on the stream, which must belong to the current device. */
+#define MPT_LINEAR_CE_MAX_V (1 << 26)
+int mpt_linear_ce_workspace_bytes(int N, int V, int H, int want_dx, int want_dW, int row_block, size_t *bytes_out);
+int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uint16_t *W_dev, int ldw, const int32_t *labels_dev,
+                  float S, int row_block, uint16_t *dx_dev, int lddx, uint16_t *dW_dev, int lddw, float *row_loss_dev,
+                  float *loss_dev, uint32_t *bad_labels_dev, uint32_t *nonfinite_flag_dev, uint32_t *status_dev,
+                  void *workspace_dev, size_t workspace_bytes, void *cuda_stream);
+
 /* mpt_softmax_ce without the caller-provided scratch.  (The paper has no counterpart:
  * this entry point exists for the sake of callers, not of the method.)
  *

@@ -40,6 +40,7 @@ EXPORTS = ["mpt_workspace_bytes", "mpt_create", "mpt_workspace_bytes_opt", "mpt_
            "mpt_lstm_forward", "mpt_lstm_backward", "mpt_lstm_cell_forward", "mpt_lstm_cell_backward", "mpt_bias_grad",
            "mpt_add_f16",
            "mpt_layernorm_forward", "mpt_layernorm_workspace_bytes", "mpt_layernorm_backward",
+           "mpt_linear_ce_workspace_bytes", "mpt_linear_ce",
            "mpt_dp_shard", "mpt_dp_step_flat", "mpt_dp_alloc", "mpt_dp_free", "mpt_dp_export", "mpt_dp_open", "mpt_dp_close",
            "mpt_dp_layout_of", "mpt_dp_attach", "mpt_dp_step_flat_opt", "mpt_dp_norm_flat", "mpt_dp_norm",
            "mpt_workspace_bytes_dp", "mpt_create_dp", "mpt_state_range", "mpt_dp_overlap_events", "mpt_dp_overlap_attach",
@@ -160,6 +161,8 @@ def lib() -> C.CDLL:
     L.mpt_layernorm_forward.argtypes = [i32, i32, vp, i32, vp, vp, f32, vp, i32, vp, vp, vp]
     L.mpt_layernorm_workspace_bytes.argtypes = [i32, i32, C.POINTER(sz)]
     L.mpt_layernorm_backward.argtypes = [i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+    L.mpt_linear_ce_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, C.POINTER(sz)]
+    L.mpt_linear_ce.argtypes = [i32, i32, i32, vp, i32, vp, i32, vp, f32, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
     L.mpt_dp_shard.argtypes = [sz, i32, i32, C.POINTER(sz), C.POINTER(sz)]
     L.mpt_dp_step_flat.argtypes = [vp, vp, vp, vp, vp, sz, i32, i32, f32, f32, f32, vp, vp]
     L.mpt_dp_step_flat_opt.argtypes = [C.POINTER(Optimizer), vp, vp, vp, vp, vp, vp, sz, i32, i32, f32, f32, f32, vp, vp, vp, vp]
@@ -578,6 +581,24 @@ def mpt_layernorm_backward(rows, cols, dy, lddy, x, ldx, gamma16, mean, rstd, dx
                              (nonfinite_flag, 4), (workspace, 1)))
     _check(lib().mpt_layernorm_backward(rows, cols, _at(dy), lddy, _at(x), ldx, _at(gamma16), _at(mean), _at(rstd), _at(dx), lddx,
                                         _at(dgamma16), _at(dbeta16), _at(nonfinite_flag), _at(workspace), workspace.numel(), st))
+
+
+# ------------------------------------------------------------ vocabulary head with its loss
+
+def mpt_linear_ce_workspace_bytes(N, V, H, want_dx=True, want_dW=True, row_block=0) -> int:
+    out = C.c_size_t(0)
+    _check(lib().mpt_linear_ce_workspace_bytes(N, V, H, int(bool(want_dx)), int(bool(want_dW)), row_block, C.byref(out)))
+    return int(out.value)
+
+
+def mpt_linear_ce(N, V, H, x, ldx, W, ldw, labels, S, row_loss, loss, dx, lddx, dW, lddw, workspace, row_block=0, bad_labels=None,
+                  nonfinite_flag=None, status=None, stream=None):
+    """dx and dW may be None (not wanted).  workspace: a uint8 tensor of at least mpt_linear_ce_workspace_bytes(...)."""
+    st = _stream_of(stream, ((x, 2), (W, 2), (labels, 4), (row_loss, 4), (loss, 4), (dx, 2), (dW, 2), (workspace, 1), (bad_labels, 4),
+                             (nonfinite_flag, 4), (status, 4)))
+    _check(lib().mpt_linear_ce(N, V, H, _at(x), ldx, _at(W), ldw, _at(labels), S, row_block, _at(dx), lddx, _at(dW), lddw,
+                               _at(row_loss), _at(loss), _at(bad_labels), _at(nonfinite_flag), _at(status), _at(workspace),
+                               workspace.numel(), st))
 
 
 class LstmLayer:

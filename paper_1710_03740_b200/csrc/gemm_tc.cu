@@ -64,6 +64,10 @@ struct TcParams {
     float *partial;
     int ldp;
     LstmEpi lstm;   // read only by the LSTM instantiations of the kernel
+    float alpha;    // factor on the FP32 sum before rounding
+    float *acc32;   // FP32 sums kept over several launches (ProductExtra), or null
+    int ldacc, acc_add, acc_store;
+    CeEpi ce;       // read only by the softmax instantiations
 };
 
 __device__ __forceinline__ void tile_coords(const TcParams &p, int tile, int &mb, int &nb)
@@ -93,7 +97,7 @@ struct EpiCfg {
     static constexpr int THREADS = 64 + 128 * SETS;
 };
 
-template <bool A_MN, bool B_MN, int BLOCK_N, bool LSTM = false, bool WIDE = false>
+template <bool A_MN, bool B_MN, int BLOCK_N, bool LSTM = false, bool WIDE = false, bool CE = false>
 __global__ void __launch_bounds__(EpiCfg<LSTM || WIDE>::THREADS, 1)
 k_gemm_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const TcParams p)
 {
@@ -257,13 +261,22 @@ k_gemm_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
                 constexpr int NCH = BLOCK_N / 64;                          // this set's half of the tile's columns
                 epilogue_lstm_tile(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * BLOCK_N + set * NCH * 32), NCH,
                                    nb * BLOCK_N + set * NCH * 32, p.N, row, row_ok, crow, p.lstm);
+            } else if constexpr (CE) {
+                constexpr int COLS = BLOCK_N / EpiCfg<LSTM || WIDE>::SETS;      // this set's columns: whole groups of 128
+                static_assert(COLS % 128 == 0, "a softmax group belongs to one thread");
+                const int label = row_ok ? p.ce.labels[row] : -1;
+                int unused = 0;
+#pragma unroll 1
+                for (int c = ((warp - 2) >> 2) * COLS, k = 0; k < COLS / 128; k++, c += 128)
+                    epilogue_ce_group<false>(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * BLOCK_N + c), nb * BLOCK_N + c, p.N,
+                                             mb * BLOCK_M + q * 32, p.M, crow, p.ce, label, 0u, nullptr, unused);
             } else {
                 // two register sets: the tensor-memory load of the next 32 columns is in flight while the
                 // current ones are rounded and stored
                 constexpr int NCHW = BLOCK_N / 32 / EpiCfg<LSTM || WIDE>::SETS;
                 const int c_begin = ((warp - 2) >> 2) * NCHW, c_end = c_begin + NCHW;
                 const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * BLOCK_N);
-                auto finish = [&](const uint32_t (&r)[32], int c) {
+                auto finish = [&](uint32_t (&r)[32], int c) {
                     const int col0 = nb * BLOCK_N + c * 32;
                     if (p.split_k > 1) {
                         // raw FP32 partial sums; ldp is a multiple of 32, so a started chunk is always whole
@@ -275,6 +288,15 @@ k_gemm_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
                                                      __uint_as_float(r[4 * v + 2]), __uint_as_float(r[4 * v + 3]));
                         }
                     } else if (row_ok && col0 < p.N) {
+                        if (p.acc32) {       // ldacc is a multiple of 32: a started chunk is whole
+                            float *acc = p.acc32 + (size_t)row * p.ldacc + col0;
+                            if (p.acc_add) add_acc32(r, acc);
+                            if (p.acc_store) {
+                                store_acc32(r, acc);
+                                return;
+                            }
+                        }
+                        scale32(r, p.alpha);
                         epilogue_store32(r, crow, mrow, col0, p.N, p.relu != 0, bad);
                     }
                 };
@@ -313,7 +335,7 @@ k_gemm_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
 __global__ void __launch_bounds__(256) k_splitk_reduce(const float *__restrict__ partial, int split_k, int M, int N,
                                                        int ldp, uint16_t *__restrict__ C, int ldc, int relu,
                                                        const uint16_t *__restrict__ mask, int ldmask,
-                                                       uint32_t *nonfinite_flag)
+                                                       uint32_t *nonfinite_flag, float alpha)
 {
     pdl_trigger();
     pdl_wait();
@@ -332,7 +354,7 @@ __global__ void __launch_bounds__(256) k_splitk_reduce(const float *__restrict__
         }
         const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
         for (int e = 0; e < 8 && col + e < N; e++) {
-            float s = v[e];
+            float s = __fmul_rn(v[e], alpha);
             if (relu) s = (s > 0.0f || s != s) ? s : 0.0f;
             uint32_t h = (uint32_t)__half_as_ushort(__float2half_rn(s));
             if (mask) {
@@ -349,13 +371,13 @@ __global__ void __launch_bounds__(256) k_splitk_reduce(const float *__restrict__
 thread_local int g_last_gemm_launches = 1;
 
 cudaError_t launch_splitk_reduce(const float *partial, int split_k, int M, int N, int ldp, uint16_t *C, int ldc, bool relu,
-                                 const uint16_t *mask, int ldmask, uint32_t *nonfinite_flag, cudaStream_t st)
+                                 const uint16_t *mask, int ldmask, uint32_t *nonfinite_flag, cudaStream_t st, float alpha)
 {
     const size_t work = (size_t)M * ((N + 7) / 8);
     size_t blocks = (work + 255) / 256;
     if (blocks > 148 * 16) blocks = 148 * 16;
     MPT_LAUNCH(k_splitk_reduce, dim3((unsigned)blocks), dim3(256), 0, st, partial, split_k, M, N, ldp, C, ldc, relu ? 1 : 0, mask, ldmask,
-               nonfinite_flag);
+               nonfinite_flag, alpha);
     g_last_gemm_launches = 2;
     return cudaGetLastError();
 }
@@ -407,13 +429,13 @@ bool tc_gemm_supported(int op, int M, int N, int K, const void *A, int lda, cons
     return true;
 }
 
-template <bool A_MN, bool B_MN, int BN, bool LSTM = false, bool WIDE = false>
+template <bool A_MN, bool B_MN, int BN, bool LSTM = false, bool WIDE = false, bool CE = false>
 static cudaError_t launch_variant(const CUtensorMap &ta, const CUtensorMap &tb, const TcParams &p, int grid,
                                   cudaStream_t st)
 {
     static bool configured[kMaxDevices] = {};
     constexpr int SMEM_BYTES = TileCfg<BN>::SMEM_BYTES;
-    auto kern = k_gemm_tc<A_MN, B_MN, BN, LSTM, WIDE>;
+    auto kern = k_gemm_tc<A_MN, B_MN, BN, LSTM, WIDE, CE>;
     const int dev = current_device_slot();
     if (dev < 0) return cudaErrorInvalidDevice;
     if (!configured[dev]) {
@@ -444,6 +466,10 @@ static cudaError_t launch_bn(int op, int M, int N, int K, const uint16_t *A, int
     int units = p.tiles_m * p.tiles_n * p.split_k;
     int grid = units < 148 ? units : 148;
     cudaError_t e;
+    if constexpr (BN >= 128) {
+        // softmax epilogue: 128 columns per set of epilogue warps, two sets on the wide tile
+        if (p.ce.stats) return launch_variant<false, false, BN, false, BN == 256, true>(ta, tb, p, grid, st);
+    }
     // two epilogue warp sets when a CTA's whole main loop is short (see EpiCfg)
     const long kblocks = ((long)(units + 147) / 148) * ((K + BLOCK_K - 1) / BLOCK_K / p.split_k);
     const bool wide = kblocks <= 160;
@@ -452,7 +478,8 @@ static cudaError_t launch_bn(int op, int M, int N, int K, const uint16_t *A, int
     else if (op == MPT_OP_DGRAD) e = wide ? launch_variant<false, true, BN, false, true>(ta, tb, p, grid, st) : launch_variant<false, true, BN>(ta, tb, p, grid, st);
     else e = wide ? launch_variant<true, true, BN, false, true>(ta, tb, p, grid, st) : launch_variant<true, true, BN>(ta, tb, p, grid, st);
     if (e != cudaSuccess || p.split_k == 1) return e;
-    return launch_splitk_reduce(p.partial, p.split_k, M, N, p.ldp, p.C, p.ldc, p.relu != 0, p.mask, p.ldmask, p.nonfinite_flag, st);
+    return launch_splitk_reduce(p.partial, p.split_k, M, N, p.ldp, p.C, p.ldc, p.relu != 0, p.mask, p.ldmask, p.nonfinite_flag, st,
+                                p.alpha);
 }
 
 // Tile width and split factor for the single-CTA kernel.  Cost model in tensor-pipe cycles: a
@@ -466,7 +493,8 @@ static cudaError_t launch_bn(int op, int M, int N, int K, const uint16_t *A, int
 // stays in L2 (about 64 bytes per cycle and SM).  Calibrated with launches replayed from a CUDA
 // graph on 2048x1024x8192, 1024x1024x4096, 512x256x4096 and the tiny-MLP products.  The split
 // is only considered when a workspace is available.
-void tc_gemm_plan(int M, int N, int K, size_t ws_bytes, int *bn_out, int *split_out, size_t *ws_needed, double *cost_out)
+void tc_gemm_plan(int M, int N, int K, size_t ws_bytes, int *bn_out, int *split_out, size_t *ws_needed, double *cost_out,
+                  int max_split)
 {
     const long tm = (M + BLOCK_M - 1) / BLOCK_M;
     const int nkb = (K + BLOCK_K - 1) / BLOCK_K;
@@ -476,7 +504,7 @@ void tc_gemm_plan(int M, int N, int K, size_t ws_bytes, int *bn_out, int *split_
         if (bn < 256 && N <= bn) continue;
         const long tiles = tm * ((N + bn - 1) / bn);
         const double cyc = bn == 256 ? 600.0 : (bn == 128 ? 437.0 : 450.0);
-        for (int s = 1; s <= 8; s++) {
+        for (int s = 1; s <= max_split; s++) {
             if (s > 1 && (nkb / s < 8)) break;
             const size_t need = s > 1 ? (size_t)s * M * (((size_t)N + 31) / 32 * 32) * 4 : 0;
             if (need > ws_bytes) break;
@@ -516,11 +544,17 @@ bool tc_choose_pair(int M, int N, int K, size_t ws_bytes, size_t *ws_needed)
 
 cudaError_t launch_gemm_tc(int op, int M, int N, int K, const uint16_t *A, int lda, const uint16_t *B, int ldb,
                            uint16_t *C, int ldc, bool relu, const uint16_t *mask, int ldmask, uint32_t *nonfinite_flag,
-                           uint32_t *status, cudaStream_t st, float *splitk_ws, size_t splitk_ws_bytes, const LstmEpi *lstm)
+                           uint32_t *status, cudaStream_t st, float *splitk_ws, size_t splitk_ws_bytes, const LstmEpi *lstm,
+                           const ProductExtra *extra)
 {
     g_last_gemm_launches = 1;
+    const ProductExtra x = extra ? *extra : ProductExtra{};
     TcParams p;
     p.lstm = LstmEpi{};
+    p.alpha = x.alpha;
+    p.acc32 = x.acc32; p.ldacc = x.ldacc; p.acc_add = x.acc_add; p.acc_store = x.acc_store;
+    p.ce = x.ce ? *x.ce : CeEpi{};
+    if (x.ce || x.acc32) splitk_ws = nullptr;      // both need the whole sum of a tile in one place
     if (lstm) {   // gate epilogue: forward products only, never split (the epilogue needs the whole sum)
         if (op != MPT_OP_FWD || (N & 31) != 0) return cudaErrorInvalidValue;
         p.lstm = *lstm;
@@ -533,7 +567,8 @@ cudaError_t launch_gemm_tc(int op, int M, int N, int K, const uint16_t *A, int l
     p.nonfinite_flag = nonfinite_flag;
     p.status = status;
     int bn = 256, split = 1;
-    tc_gemm_plan(M, N, K, (splitk_ws && (((uintptr_t)splitk_ws) & 15) == 0) ? splitk_ws_bytes : 0, &bn, &split, nullptr);
+    tc_gemm_plan(M, N, K, (splitk_ws && (((uintptr_t)splitk_ws) & 15) == 0) ? splitk_ws_bytes : 0, &bn, &split, nullptr, nullptr, x.max_split);
+    if (x.ce && bn < 128) bn = 128;
     p.split_k = split;
     p.partial = splitk_ws;
     p.ldp = (N + 31) / 32 * 32;

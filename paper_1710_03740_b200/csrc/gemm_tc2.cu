@@ -80,6 +80,10 @@ struct Params {
     int tma_store;                   // output of whole and half tiles through shared memory and tensor stores
     int hint_a, hint_b;              // L2 eviction priority of the operand loads (0 normal, 1 last, 2 first)
     LstmEpi lstm;                    // read only by the LSTM instantiation of the kernel
+    float alpha;                     // factor on the FP32 sum before rounding
+    float *acc32;                    // FP32 sums kept over several launches (ProductExtra), or null
+    int ldacc, acc_add, acc_store;
+    CeEpi ce;                        // read only by the softmax instantiation
 };
 
 struct Unit {
@@ -151,7 +155,7 @@ struct EpiCfg {
     static constexpr int THREADS = 64 + 128 * SETS;
 };
 
-template <bool A_MN, bool B_MN, bool LSTM = false, bool WIDE = false>
+template <bool A_MN, bool B_MN, bool LSTM = false, bool WIDE = false, bool CE = false>
 __global__ void __launch_bounds__(EpiCfg<LSTM || WIDE>::THREADS, 1)
 k_gemm_tc2(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
            const __grid_constant__ CUtensorMap tmBh, const __grid_constant__ CUtensorMap tmC, const Params p)
@@ -342,6 +346,13 @@ k_gemm_tc2(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                 const int set = (warp - 2) >> 2, nch = w.width / 64;       // this set's half of the unit's columns
                 epilogue_lstm_tile(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * TILE_N + set * nch * 32), nch,
                                    w.nb * TILE_N + w.n_off + set * nch * 32, p.N, row, row_ok, crow, p.lstm);
+            } else if constexpr (CE) {
+                const int label = row_ok ? p.ce.labels[row] : -1;
+#pragma unroll 1
+                for (int c = 0; c < w.width; c += 128)
+                    epilogue_ce_group<true>(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * TILE_N + c),
+                                            w.nb * TILE_N + w.n_off + c, p.N, w.mb * (2 * CTA_M) + (int)rank * CTA_M + q * 32, p.M, crow,
+                                            p.ce, label, epi_stage + (uint32_t)((warp - 2) * 2 * EPI_BOX_BYTES), &tmC, boxes_sent);
             } else if (w.tail_slot >= 0) {
                 // unit of the split tail: the raw 256x256 FP32 block of this part (all rows, all columns)
                 float *prow = p.tail_partial + (size_t)w.tail_slot * (2 * CTA_M * TILE_N) +
@@ -393,7 +404,7 @@ k_gemm_tc2(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     __syncwarp();
                     const int colb = w.nb * TILE_N + w.n_off + bx * 64;
                     epilogue_box_store(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * TILE_N + bx * 64), box, &tmC, row0,
-                                       colb, p.M, p.N, p.relu != 0, mrow, row_ok, acc_bits);
+                                       colb, p.M, p.N, p.relu != 0, mrow, row_ok, acc_bits, p.alpha);
                 }
                 bad |= nonfinite_any(acc_bits);
             } else {
@@ -404,7 +415,18 @@ k_gemm_tc2(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     tc_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * TILE_N + c * 32), r);
                     tc_wait_ld();
                     const int col0 = w.nb * TILE_N + w.n_off + c * 32;
-                    if (row_ok && col0 < p.N) epilogue_store32(r, crow, mrow, col0, p.N, p.relu != 0, bad);
+                    if (row_ok && col0 < p.N) {
+                        if (p.acc32) {       // ldacc is a multiple of 32: a started chunk is whole
+                            float *acc = p.acc32 + (size_t)row * p.ldacc + col0;
+                            if (p.acc_add) add_acc32(r, acc);
+                            if (p.acc_store) {
+                                store_acc32(r, acc);
+                                continue;
+                            }
+                        }
+                        scale32(r, p.alpha);
+                        epilogue_store32(r, crow, mrow, col0, p.N, p.relu != 0, bad);
+                    }
                 }
             }
             tc_fence_before();
@@ -453,7 +475,7 @@ __global__ void __launch_bounds__(256) k_tail_reduce(const Params p, int first_t
         }
         const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
         for (int e = 0; e < 8 && col + e < p.N; e++) {
-            float s = v[e];
+            float s = __fmul_rn(v[e], p.alpha);
             if (p.relu) s = (s > 0.0f || s != s) ? s : 0.0f;
             uint32_t h = (uint32_t)__half_as_ushort(__float2half_rn(s));
             if (p.mask) {
@@ -467,12 +489,12 @@ __global__ void __launch_bounds__(256) k_tail_reduce(const Params p, int first_t
     if (p.nonfinite_flag && __any_sync(0xFFFFFFFFu, bad) && (threadIdx.x & 31) == 0) atomicOr(p.nonfinite_flag, 1u);
 }
 
-template <bool A_MN, bool B_MN, bool LSTM = false, bool WIDE = false>
+template <bool A_MN, bool B_MN, bool LSTM = false, bool WIDE = false, bool CE = false>
 static cudaError_t launch_variant(const CUtensorMap &ta, const CUtensorMap &tb, const CUtensorMap &tbh, const CUtensorMap &tc,
                                   Params p, cudaStream_t st)
 {
     static int max_pairs_dev[kMaxDevices] = {};     // 0 = this device not configured yet
-    auto kern = k_gemm_tc2<A_MN, B_MN, LSTM, WIDE>;
+    auto kern = k_gemm_tc2<A_MN, B_MN, LSTM, WIDE, CE>;
     const int dev = current_device_slot();
     if (dev < 0) return cudaErrorInvalidDevice;
     cudaLaunchConfig_t cfg = {};
@@ -610,10 +632,13 @@ void tc2_split_plan(int M, int N, int K, size_t ws_bytes, int *split_out, size_t
 
 cudaError_t launch_gemm_tc2(int op, int M, int N, int K, const uint16_t *A, int lda, const uint16_t *B, int ldb,
                             uint16_t *C, int ldc, bool relu, const uint16_t *mask, int ldmask, uint32_t *nonfinite_flag,
-                            uint32_t *status, cudaStream_t st, const LstmEpi *lstm, void *splitk_ws, size_t splitk_ws_bytes)
+                            uint32_t *status, cudaStream_t st, const LstmEpi *lstm, void *splitk_ws, size_t splitk_ws_bytes,
+                            const ProductExtra *extra)
 {
     using namespace pair;
     g_last_gemm_launches = 1;
+    const ProductExtra x = extra ? *extra : ProductExtra{};
+    if (x.ce || x.acc32) splitk_ws = nullptr;      // both need the whole sum of a tile in one place
     CUtensorMap ta, tb, tbh;
     bool ok;
     if (op == MPT_OP_WGRAD) ok = tc_encode_map(&ta, A, (uint64_t)K, (uint64_t)M, (uint64_t)lda, 64, BLOCK_K);
@@ -627,7 +652,8 @@ cudaError_t launch_gemm_tc2(int op, int M, int N, int K, const uint16_t *A, int 
         tbh = tb;
     }
     CUtensorMap tcm;      // the output, in boxes of 32 rows x 64 columns
-    ok = ok && tc_encode_map(&tcm, C, (uint64_t)M, (uint64_t)N, (uint64_t)ldc, 64, 32);
+    if (x.ce && !x.ce->store) tcm = ta;            // never stored through
+    else ok = ok && tc_encode_map(&tcm, C, (uint64_t)M, (uint64_t)(x.ce ? (N + 7) / 8 * 8 : N), (uint64_t)ldc, 64, 32);
     if (!ok) return cudaErrorInvalidValue;
     Params p;
     p.M = M; p.N = N; p.K = K;
@@ -635,6 +661,10 @@ cudaError_t launch_gemm_tc2(int op, int M, int N, int K, const uint16_t *A, int 
     // tensor stores of the output: whole groups of 8 columns only (the mask and the inf/NaN vote work on such groups);
     // MPT_TMA_STORE=0 selects the per-lane 16-byte stores for comparisons
     { const char *x = getenv("MPT_TMA_STORE"); p.tma_store = (N % 8 == 0) && (x ? atoi(x) != 0 : true); }
+    p.alpha = x.alpha;
+    p.acc32 = x.acc32; p.ldacc = x.ldacc; p.acc_add = x.acc_add; p.acc_store = x.acc_store;
+    if (x.acc32) p.tma_store = 0;
+    p.ce = x.ce ? *x.ce : CeEpi{};
     p.mask = mask; p.ldmask = ldmask;
     p.relu = relu ? 1 : 0;
     p.nonfinite_flag = nonfinite_flag;
@@ -684,6 +714,10 @@ cudaError_t launch_gemm_tc2(int op, int M, int N, int K, const uint16_t *A, int 
         p.lstm = *lstm;
         return launch_variant<false, false, true>(ta, tb, tbh, tcm, p, st);
     }
+    if (x.ce) {
+        if (op != MPT_OP_FWD) return cudaErrorInvalidValue;
+        return launch_variant<false, false, false, false, true>(ta, tb, tbh, tcm, p, st);
+    }
     // two epilogue warp sets when a cluster's whole main loop is short (see EpiCfg)
     const long units = (long)p.tiles_m * p.tiles_n * p.split_k;
     const long kblocks = ((units + 73) / 74) * ((K + BLOCK_K - 1) / BLOCK_K / p.split_k);
@@ -693,7 +727,7 @@ cudaError_t launch_gemm_tc2(int op, int M, int N, int K, const uint16_t *A, int 
     else if (op == MPT_OP_DGRAD) e = wide ? launch_variant<false, true, false, true>(ta, tb, tbh, tcm, p, st) : launch_variant<false, true>(ta, tb, tbh, tcm, p, st);
     else e = wide ? launch_variant<true, true, false, true>(ta, tb, tbh, tcm, p, st) : launch_variant<true, true>(ta, tb, tbh, tcm, p, st);
     if (e != cudaSuccess || p.split_k == 1) return e;
-    return launch_splitk_reduce(p.partial, p.split_k, M, N, p.ldp, C, ldc, relu, mask, ldmask, nonfinite_flag, st);
+    return launch_splitk_reduce(p.partial, p.split_k, M, N, p.ldp, C, ldc, relu, mask, ldmask, nonfinite_flag, st, x.alpha);
 }
 
 }  // namespace mpt

@@ -69,6 +69,7 @@ struct Params {
     uint32_t *nonfinite_flag;
     uint32_t *status;
     int tiles_m, tiles_n;
+    float alpha;                    // factor on the FP32 sum before rounding
 };
 
 __device__ __forceinline__ void report(const Params &p, volatile uint32_t *abort_flag, uint32_t code)
@@ -335,6 +336,7 @@ k_gemm_tc4(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     }
 #pragma unroll
                     for (int e = 0; e < 32; e++) r[e] = __float_as_uint(sum[e]);
+                    scale32(r, p.alpha);
                     const int col0 = nb * TILE_N + g * W + set * WCOLS + c * 32;
                     epilogue_store32_coalesced(r, base_ptr + RECV_BYTES + SEND_BYTES + w * EPI_STAGE_BYTES, p.C, p.ldc, p.mask, p.ldmask,
                                                mb * (2 * CTA_M) + (int)half * CTA_M + q * 32, col0, p.M, p.N, p.relu != 0, bad);
@@ -452,7 +454,7 @@ int tc4_split_for(int M, int N, int K)
 
 cudaError_t launch_gemm_tc4(int op, int M, int N, int K, const uint16_t *A, int lda, const uint16_t *B, int ldb,
                             uint16_t *C, int ldc, bool relu, const uint16_t *mask, int ldmask, uint32_t *nonfinite_flag,
-                            uint32_t *status, cudaStream_t st, int split)
+                            uint32_t *status, cudaStream_t st, int split, float alpha)
 {
     using namespace quad;
     g_last_gemm_launches = 1;
@@ -474,6 +476,7 @@ cudaError_t launch_gemm_tc4(int op, int M, int N, int K, const uint16_t *A, int 
     p.status = status;
     p.tiles_m = (M + 2 * CTA_M - 1) / (2 * CTA_M);
     p.tiles_n = (N + TILE_N - 1) / TILE_N;
+    p.alpha = alpha;
     if (split == 2) {
         if (op == MPT_OP_FWD) return launch_variant<false, false, 2>(ta, tb, p, st);
         if (op == MPT_OP_DGRAD) return launch_variant<false, true, 2>(ta, tb, p, st);

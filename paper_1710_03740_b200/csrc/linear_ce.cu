@@ -1,0 +1,303 @@
+// Linear layer over a large vocabulary fused with the softmax cross-entropy of its outputs (paper sections 3.2,
+// 3.3: FP16 operands, FP32 sums and softmax arithmetic, gradient multiplied by S / N before it is rounded), without
+// a logits matrix and without rounding the logits:
+//
+//   z = x . W^T in FP32 ;  loss_i = log sum_v exp(z_iv) - z_i,y(i)
+//   dx = rn16(S / N * sum_v (p_iv - [v = y(i)]) W_v) ;  dW_v = rn16(S / N * sum_i (p_iv - [v = y(i)]) x_i)
+//
+// Work: 2 N V H for the losses, 6 N V H with both gradients; bound: the tensor pipe (for few rows: reading W and
+// writing dW).  The rows go through in blocks of R; per block
+//   1  the logits product with a softmax epilogue: the accumulators of 128 classes of a row become FP16
+//      exponentials relative to their own maximum (CeEpi), with their FP32 sum, and the label's FP32 logit
+//   2  k_ce_combine: log2 of the row's whole sum, and the row's loss (and x without the ignored rows, for step 5)
+//   3  k_ce_rescale: exponentials -> 2^14 (p - [v = y]) in place
+//   4  dx = product of those with W, 5 dW = product of their transpose with x, both with the factor S / N * 2^-14
+//      in the epilogue
+// Keeping the exponentials costs 2 bytes a logit of a block and step 3 (4 bytes a logit through HBM: 143/H of the
+// products' time), computing them a second time would cost a fourth product (1/3).  FP16 keeps them, and p, to
+// 2^-12 of the value whatever S and N: the scale 2^14 leaves 2^-38 of a group's largest term (resp. of 1) above
+// zero, where p * S / N in FP16 would lose p below 2^-24 N / S.  Over several row blocks dW is summed in FP32.
+#include <math.h>
+
+#include "mpt_common.cuh"
+
+namespace mpt {
+namespace {
+
+constexpr int kGroup = 128;           // classes of one softmax group (CeEpi)
+constexpr int kDefaultRows = 4096;    // rows of a block when the caller does not choose
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Row sums from the group sums: lse2 = log2 sum_g s_g 2^(-b_g), and the row's loss.  Four rows per CTA (a 32-byte
+// sector of `stats` holds one group of four rows), 64 threads a row; fixed order.
+// xs (null: not wanted) receives x with the rows of ignored labels as zeros: what a padding row holds, NaN
+// perhaps, must not meet its zero gradient in dW's product.
+__global__ void __launch_bounds__(256) k_ce_combine(const float2 *__restrict__ stats, int R, int V, int groups,
+                                                    const int32_t *__restrict__ labels, const float *__restrict__ zlabel,
+                                                    float *__restrict__ lse2, float *__restrict__ row_loss, uint32_t *bad_labels,
+                                                    const uint16_t *__restrict__ x, int ldx, int H, uint16_t *__restrict__ xs)
+{
+    pdl_trigger();
+    pdl_wait();
+    __shared__ float2 red[8][4];
+    if (xs) {
+        const int xrow = blockIdx.x * 4 + (threadIdx.x >> 6);
+        if (xrow < R) {
+            const bool live = (unsigned)labels[xrow] < (unsigned)V;
+            const uint4 *src = (const uint4 *)(x + (size_t)xrow * ldx);
+            uint4 *dst = (uint4 *)(xs + (size_t)xrow * H);
+            for (int i = threadIdx.x & 63; i < H / 8; i += 64) dst[i] = live ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+    const int r = threadIdx.x & 3, row = blockIdx.x * 4 + r;
+    float m = -INFINITY, s = 0.0f;
+    if (row < R) {
+        for (int g = threadIdx.x >> 2; g < groups; g += 64) {
+            const float2 t = stats[(size_t)g * R + row];
+            const float e = -t.y, mn = fmaxf(m, e);         // b is finite, or NaN or -inf where the logits were not
+            s = s * ex2(m - mn) + t.x * ex2(e - mn);
+            m = mn;
+        }
+    }
+    // (m, s) pairs with m = -inf hold no terms yet
+    auto join = [](float &m1, float &s1, float m2, float s2) {
+        const float mn = fmaxf(m1, m2);
+        s1 = (m1 == -INFINITY ? 0.0f : s1 * ex2(m1 - mn)) + (m2 == -INFINITY ? 0.0f : s2 * ex2(m2 - mn));
+        m1 = mn;
+    };
+#pragma unroll
+    for (int o = 4; o < 32; o <<= 1) {
+        const float m2 = __shfl_xor_sync(0xFFFFFFFFu, m, o), s2 = __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        join(m, s, m2, s2);
+    }
+    if ((threadIdx.x & 31) < 4) red[threadIdx.x >> 5][r] = make_float2(m, s);
+    __syncthreads();
+    if (threadIdx.x < 4 && row < R) {
+        m = red[0][r].x;
+        s = red[0][r].y;
+#pragma unroll
+        for (int w = 1; w < 8; w++) join(m, s, red[w][r].x, red[w][r].y);
+        const int y = labels[row];
+        const bool good = y >= 0 && y < V;
+        lse2[row] = m + log2f(s);
+        if (good) row_loss[row] = (float)(((double)m + log2((double)s)) * 0.69314718055994530942 - (double)zlabel[row]);
+        else row_loss[row] = 0.0f;                      // contributes neither loss nor gradient
+        if (!good && bad_labels) atomicAdd(bad_labels, 1u);
+    }
+}
+
+// e -> 2^14 (p - [v = y]) in place.  A warp takes 2048 columns of one row, 16 bytes a lane, all loads ahead of the
+// first use; the eight warps of a CTA take neighbouring rows, which share the sectors of `stats`.
+__global__ void __launch_bounds__(256) k_ce_rescale(uint16_t *__restrict__ e16, int ld, const float2 *__restrict__ stats, int R,
+                                                    int V, const int32_t *__restrict__ labels, const float *__restrict__ zlabel,
+                                                    const float *__restrict__ lse2)
+{
+    pdl_trigger();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, row = blockIdx.y * 8 + (threadIdx.x >> 5);
+    if (row >= R) return;
+    const int col0 = blockIdx.x * 2048 + lane * 8;
+    uint16_t *er = e16 + (size_t)row * ld;
+    const int y = labels[row];
+    const bool good = y >= 0 && y < V;
+    uint4 v[8];
+    float f[8];
+    const float lse = lse2[row];
+#pragma unroll
+    for (int u = 0; u < 8; u++) {
+        const int col = col0 + u * 256;
+        if (good && col < ld) {
+            v[u] = *(const uint4 *)(er + col);
+            f[u] = stats[(size_t)(col / kGroup) * R + row].y;
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < 8; u++) {
+        const int col = col0 + u * 256;
+        if (col >= ld) continue;
+        uint32_t w[4] = {0u, 0u, 0u, 0u};
+        if (good) {
+            const uint32_t x[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+            const float k = ex2((14.0f - f[u]) - lse);
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                const float2 t = __half22float2(*(const __half2 *)&x[q]);
+                const __half2 h = __floats2half2_rn(t.x * k, t.y * k);
+                w[q] = *(const uint32_t *)&h;
+            }
+            if (y - col >= 0 && y - col < 8) {           // the label's element from its FP32 logit
+                const float p = ex2(fmaf(zlabel[row], 1.4426950408889634f, -lse));
+                const uint32_t h = (uint32_t)__half_as_ushort(__float2half_rn((p - 1.0f) * 16384.0f));
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    if (((y - col) >> 1) == q) w[q] = ((y - col) & 1) ? ((w[q] & 0x0000FFFFu) | (h << 16)) : ((w[q] & 0xFFFF0000u) | h);
+                }
+            }
+        }
+        *(uint4 *)(er + col) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// Where things are in the workspace (256-byte aligned offsets).
+struct Plan {
+    int R, blocks;        // rows of a block, number of blocks
+    int lde;              // pitch of the exponentials
+    int groups;
+    int ldacc;
+    size_t e16, stats, lse2, zlabel, xs, splitk, splitk_bytes, acc32, total;
+};
+
+// The split of dx's contraction over the vocabulary: for few rows the product has few tiles and reading W is what
+// takes time, so as many SMs as possible have to take part.
+constexpr int kDxSplit = 64;
+
+size_t product_scratch(int op, int M, int N, int K, int max_split)
+{
+    if (tc4_split_for(M, N, K)) return 0;
+    size_t need = 0;
+    if (tc2_gemm_preferred(M, N, K)) return tc2_tail_ws_bytes(M, N, K);
+    int bn, split;
+    tc_gemm_plan(M, N, K, (size_t)1 << 40, &bn, &split, &need, nullptr, max_split);
+    (void)op;
+    return need;
+}
+
+Plan make_plan(int N, int V, int H, bool want_dx, bool want_dW, int row_block)
+{
+    Plan p = {};
+    p.R = row_block > 0 ? row_block : kDefaultRows;
+    if (p.R > N) p.R = N > 0 ? N : 1;
+    p.blocks = (N + p.R - 1) / p.R;
+    p.lde = (V + 7) / 8 * 8;
+    p.groups = (V + kGroup - 1) / kGroup;
+    p.ldacc = (H + 31) / 32 * 32;
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) / 256 * 256; return o; };
+    const bool grads = want_dx || want_dW;
+    p.e16 = take(grads ? (size_t)p.R * p.lde * 2 : 0);
+    p.stats = take((size_t)p.groups * p.R * sizeof(float2));
+    p.lse2 = take((size_t)p.R * sizeof(float));
+    p.zlabel = take((size_t)p.R * sizeof(float));
+    p.xs = take(want_dW ? (size_t)p.R * H * 2 : 0);
+    size_t sk = 0;
+    if (want_dx) {
+        sk = product_scratch(MPT_OP_DGRAD, p.R, H, V, kDxSplit);
+        const int rest = N - (p.blocks - 1) * p.R;          // the last block may be shorter
+        if (p.blocks > 1 && rest != p.R) {
+            const size_t s2 = product_scratch(MPT_OP_DGRAD, rest, H, V, kDxSplit);
+            sk = s2 > sk ? s2 : sk;
+        }
+    }
+    if (want_dW && p.blocks == 1) {
+        const size_t s2 = product_scratch(MPT_OP_WGRAD, V, H, p.R, 8);
+        sk = s2 > sk ? s2 : sk;
+    }
+    p.splitk_bytes = sk;
+    p.splitk = take(sk);
+    p.acc32 = take(want_dW && p.blocks > 1 ? (size_t)V * p.ldacc * sizeof(float) : 0);
+    p.total = at;
+    return p;
+}
+
+// One of the products, on the kernel the plain entry point would choose.
+cudaError_t product(int op, int M, int N, int K, const uint16_t *A, int lda, const uint16_t *B, int ldb, uint16_t *C, int ldc,
+                    const ProductExtra &x, uint32_t *nonfinite, uint32_t *status, void *ws, size_t ws_bytes, cudaStream_t st)
+{
+    if (x.ce) {
+        // 256-row tiles only where there are more than 128 rows and enough tiles for the CTA pairs
+        const long tiles = (long)((M + 255) / 256) * ((N + 255) / 256);
+        if (M > 128 && N >= 256 && tiles > 74)
+            return launch_gemm_tc2(op, M, N, K, A, lda, B, ldb, C, ldc, false, nullptr, 0, nonfinite, status, st, nullptr, nullptr, 0, &x);
+        return launch_gemm_tc(op, M, N, K, A, lda, B, ldb, C, ldc, false, nullptr, 0, nonfinite, status, st, nullptr, 0, nullptr, &x);
+    }
+    if (!x.acc32) {
+        if (const int split = tc4_split_for(M, N, K))
+            return launch_gemm_tc4(op, M, N, K, A, lda, B, ldb, C, ldc, false, nullptr, 0, nonfinite, status, st, split, x.alpha);
+    }
+    if (tc2_gemm_preferred(M, N, K))
+        return launch_gemm_tc2(op, M, N, K, A, lda, B, ldb, C, ldc, false, nullptr, 0, nonfinite, status, st, nullptr, ws, ws_bytes, &x);
+    return launch_gemm_tc(op, M, N, K, A, lda, B, ldb, C, ldc, false, nullptr, 0, nonfinite, status, st, (float *)ws, ws_bytes, nullptr, &x);
+}
+
+}  // namespace
+}  // namespace mpt
+
+using namespace mpt;
+
+extern "C" {
+
+int mpt_linear_ce_workspace_bytes(int N, int V, int H, int want_dx, int want_dW, int row_block, size_t *bytes_out)
+{
+    if (!bytes_out) return MPT_ERR_INVALID_ARG;
+    if (N < 0 || V < 1 || V > MPT_LINEAR_CE_MAX_V || H < 8 || H % 8 || row_block < 0 || row_block % 256) return MPT_ERR_SHAPE;
+    *bytes_out = make_plan(N, V, H, want_dx != 0, want_dW != 0, row_block).total;
+    return MPT_OK;
+}
+
+int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uint16_t *W_dev, int ldw, const int32_t *labels_dev,
+                  float S, int row_block, uint16_t *dx_dev, int lddx, uint16_t *dW_dev, int lddw, float *row_loss_dev,
+                  float *loss_dev, uint32_t *bad_labels_dev, uint32_t *nonfinite_flag_dev, uint32_t *status_dev,
+                  void *workspace_dev, size_t workspace_bytes, void *cuda_stream)
+{
+    if (!x_dev || !W_dev || !labels_dev || !row_loss_dev || !loss_dev || !workspace_dev) return MPT_ERR_INVALID_ARG;
+    if (!isfinite(S) || dx_dev == x_dev || dW_dev == W_dev) return MPT_ERR_INVALID_ARG;
+    if (N < 0 || V < 1 || V > MPT_LINEAR_CE_MAX_V || H < 8 || H % 8 || row_block < 0 || row_block % 256) return MPT_ERR_SHAPE;
+    if (ldx < H || ldw < H || (dx_dev && lddx < H) || (dW_dev && lddw < H)) return MPT_ERR_SHAPE;
+    const uintptr_t bits = (uintptr_t)x_dev | (uintptr_t)W_dev | (uintptr_t)dx_dev | (uintptr_t)dW_dev;
+    if ((bits & 15) || ldx % 8 || ldw % 8 || (dx_dev && lddx % 8) || (dW_dev && lddw % 8)) return MPT_ERR_SHAPE;
+    const Plan p = make_plan(N, V, H, dx_dev != nullptr, dW_dev != nullptr, row_block);
+    if (workspace_bytes < p.total || ((uintptr_t)workspace_dev & 255)) return MPT_ERR_WORKSPACE;
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    uint8_t *ws = (uint8_t *)workspace_dev;
+    uint16_t *e16 = (uint16_t *)(ws + p.e16);
+    float2 *stats = (float2 *)(ws + p.stats);
+    float *lse2 = (float *)(ws + p.lse2), *zlabel = (float *)(ws + p.zlabel);
+    uint16_t *xs = dW_dev ? (uint16_t *)(ws + p.xs) : nullptr;
+    const bool grads = dx_dev || dW_dev;
+    cudaError_t e = cudaSuccess;
+    if (bad_labels_dev) e = cudaMemsetAsync(bad_labels_dev, 0, sizeof(uint32_t), st);
+    if (e == cudaSuccess && N == 0 && dW_dev) e = cudaMemset2DAsync(dW_dev, (size_t)lddw * 2, 0, (size_t)H * 2, (size_t)V, st);
+    const float alpha = S / (float)N * (1.0f / 16384.0f);
+    for (int b = 0; b < p.blocks && e == cudaSuccess; b++) {
+        const int r0 = b * p.R, R = N - r0 < p.R ? N - r0 : p.R;
+        const uint16_t *x = x_dev + (size_t)r0 * ldx;
+        const int32_t *labels = labels_dev + r0;
+        const CeEpi ce = {labels, stats, zlabel, grads ? 1 : 0};
+        ProductExtra xl, xd, xw;
+        xl.ce = &ce;
+        e = product(MPT_OP_FWD, R, V, H, x, ldx, W_dev, ldw, grads ? e16 : nullptr, p.lde, xl, nullptr, status_dev, nullptr, 0, st);
+        if (e != cudaSuccess) break;
+        e = launch_pdl(k_ce_combine, dim3((unsigned)((R + 3) / 4)), dim3(256), 0, st, (const float2 *)stats, R, V, p.groups, labels,
+                       (const float *)zlabel, lse2, row_loss_dev + r0, bad_labels_dev, x, ldx, H, xs);
+        if (e != cudaSuccess || !grads) continue;
+        e = launch_pdl(k_ce_rescale, dim3((unsigned)((p.lde + 2047) / 2048), (unsigned)((R + 7) / 8)), dim3(256), 0, st, e16, p.lde,
+                       (const float2 *)stats, R, V, labels, (const float *)zlabel, (const float *)lse2);
+        if (e == cudaSuccess && dx_dev) {
+            xd.alpha = alpha;
+            xd.max_split = kDxSplit;
+            e = product(MPT_OP_DGRAD, R, H, V, e16, p.lde, W_dev, ldw, dx_dev + (size_t)r0 * lddx, lddx, xd, nullptr, status_dev,
+                        ws + p.splitk, p.splitk_bytes, st);
+        }
+        if (e == cudaSuccess && dW_dev) {
+            xw.alpha = alpha;
+            if (p.blocks > 1) {
+                xw.acc32 = (float *)(ws + p.acc32);
+                xw.ldacc = p.ldacc;
+                xw.acc_add = b > 0;
+                xw.acc_store = b + 1 < p.blocks;
+            }
+            e = product(MPT_OP_WGRAD, V, H, R, e16, p.lde, xs, H, dW_dev, lddw, xw, xw.acc_store ? nullptr : nonfinite_flag_dev,
+                        status_dev, ws + p.splitk, p.splitk_bytes, st);
+        }
+    }
+    if (e == cudaSuccess) e = launch_loss_mean(row_loss_dev, N, loss_dev, st);
+    return e == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -106,6 +106,28 @@ struct LstmEpi {
     int ldh;
 };
 
+// Softmax epilogue of a logits product z = x . W^T (linear_ce.cu): the FP32 accumulators of 128 neighbouring
+// classes of a row are turned into exponentials relative to their own maximum, 2^(z*log2e + b) with b = 14 -
+// max*log2e, so that the largest is 2^14 and FP16 keeps terms down to 2^-38 of it.  Their FP32 sum and b go to
+// stats[group][row], the exponentials (rounded to FP16) to the product's output, the label's logit to zlabel[row].
+struct CeEpi {
+    const int32_t *labels;    // [M]
+    float2 *stats;            // [ceil(N / 128)][M]: (sum, b)
+    float *zlabel;            // [M]
+    int store;                // 0: statistics only, nothing is written to the output
+};
+// What a product's launcher can be asked for beyond the plain call.
+struct ProductExtra {
+    float alpha = 1.0f;           // factor on the FP32 sum before it is rounded to FP16
+    // sums over several launches (the contraction cut into row blocks): add what acc32 [M, ldacc] holds, and
+    // store the FP32 sum there instead of an output (every launch but the last)
+    float *acc32 = nullptr;
+    int ldacc = 0;
+    int acc_add = 0, acc_store = 0;
+    const CeEpi *ce = nullptr;    // softmax epilogue (forward products)
+    int max_split = 8;            // single-CTA kernel: most parts the contraction may be cut into
+};
+
 // Launchers (each returns a cudaError_t from the launch; all asynchronous on `st`).
 cudaError_t launch_recast(const float *w32, uint16_t *w16, size_t n, cudaStream_t st);
 cudaError_t launch_grad_nonfinite(const uint16_t *g16, size_t n, float inv_S, uint32_t *flag,
@@ -118,6 +140,8 @@ cudaError_t launch_update(const uint16_t *g16, float *w32, float *v, uint16_t *w
 cudaError_t launch_softmax_ce(const uint16_t *z, int ldz, const int32_t *labels, int B, int C, float S,
                               uint16_t *dz, int lddz, float *row_loss, float *loss, uint32_t *bad_labels,
                               cudaStream_t st, int *n_launches, const float *S_dev = nullptr, uint32_t *kerr = nullptr);
+// *loss = mean of row_loss[0..B) in double, fixed order (softmax_ce.cu).
+cudaError_t launch_loss_mean(const float *row_loss, int B, float *loss, cudaStream_t st);
 // One warp measures its SM's clock over window_us of wall time and writes MHz to *mhz_out (clock_probe.cu).
 cudaError_t launch_clock_probe(unsigned window_us, float *mhz_out, cudaStream_t st);
 // One CTA waits, for at most limit_us, on a barrier nothing arrives on; on expiry it records
@@ -186,9 +210,9 @@ bool tc_gemm_supported(int op, int M, int N, int K, const void *A, int lda, cons
 cudaError_t launch_gemm_tc(int op, int M, int N, int K, const uint16_t *A, int lda, const uint16_t *B,
                            int ldb, uint16_t *C, int ldc, bool relu, const uint16_t *mask, int ldmask,
                            uint32_t *nonfinite_flag, uint32_t *status, cudaStream_t st, float *splitk_ws = nullptr,
-                           size_t splitk_ws_bytes = 0, const LstmEpi *lstm = nullptr);
+                           size_t splitk_ws_bytes = 0, const LstmEpi *lstm = nullptr, const ProductExtra *extra = nullptr);
 void tc_gemm_plan(int M, int N, int K, size_t ws_bytes, int *bn_out, int *split_out, size_t *ws_needed,
-                  double *cost_out = nullptr);
+                  double *cost_out = nullptr, int max_split = 8);
 // Kernel choice for a product the tensor-core path takes: true = CTA-pair kernel (possibly with a
 // split contraction), false = single-CTA kernel; ws_needed = scratch the choice would like.
 bool tc_choose_pair(int M, int N, int K, size_t ws_bytes, size_t *ws_needed);
@@ -202,11 +226,11 @@ bool tc2_gemm_preferred(int M, int N, int K);
 cudaError_t launch_gemm_tc2(int op, int M, int N, int K, const uint16_t *A, int lda, const uint16_t *B, int ldb,
                             uint16_t *C, int ldc, bool relu, const uint16_t *mask, int ldmask,
                             uint32_t *nonfinite_flag, uint32_t *status, cudaStream_t st, const LstmEpi *lstm = nullptr,
-                            void *splitk_ws = nullptr, size_t splitk_ws_bytes = 0);
+                            void *splitk_ws = nullptr, size_t splitk_ws_bytes = 0, const ProductExtra *extra = nullptr);
 // Second step of a split product: C = epilogue(partial[0] + partial[1] + ...), parts added in
 // ascending order with one rounding per add.
 cudaError_t launch_splitk_reduce(const float *partial, int split_k, int M, int N, int ldp, uint16_t *C, int ldc, bool relu,
-                                 const uint16_t *mask, int ldmask, uint32_t *nonfinite_flag, cudaStream_t st);
+                                 const uint16_t *mask, int ldmask, uint32_t *nonfinite_flag, cudaStream_t st, float alpha = 1.0f);
 // CTA-pair variant with 256x512 tiles (two accumulators fed by one stream of A; the epilogue is
 // not overlapped): less operand traffic, not faster; only on request (MPT_GEMM_FORCE_PAIR512).
 cudaError_t launch_gemm_tc3(int op, int M, int N, int K, const uint16_t *A, int lda, const uint16_t *B, int ldb,
@@ -218,7 +242,7 @@ cudaError_t launch_gemm_tc3(int op, int M, int N, int K, const uint16_t *A, int 
 int tc4_split_for(int M, int N, int K);
 cudaError_t launch_gemm_tc4(int op, int M, int N, int K, const uint16_t *A, int lda, const uint16_t *B, int ldb,
                             uint16_t *C, int ldc, bool relu, const uint16_t *mask, int ldmask,
-                            uint32_t *nonfinite_flag, uint32_t *status, cudaStream_t st, int split);
+                            uint32_t *nonfinite_flag, uint32_t *status, cudaStream_t st, int split, float alpha = 1.0f);
 size_t tc2_tail_ws_bytes(int M, int N, int K);
 // Split factor, scratch need (FP32 parts) and modelled cost
 // of the pair kernel for an output with few tiles and a long contraction; split 1 = no split.

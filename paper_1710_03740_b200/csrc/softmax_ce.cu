@@ -430,6 +430,12 @@ __global__ void __launch_bounds__(256) k_loss_mean(const float *__restrict__ row
     if (threadIdx.x == 0) *loss = (B > 0) ? (float)(red[0] / (double)B) : 0.0f;
 }
 
+cudaError_t launch_loss_mean(const float *row_loss, int B, float *loss, cudaStream_t st)
+{
+    MPT_LAUNCH(k_loss_mean, dim3(1), dim3(256), 0, st, row_loss, B, loss);
+    return cudaGetLastError();
+}
+
 template <bool VEC, bool CACHE>
 static cudaError_t launch_variant(const uint16_t *z, int ldz, const int32_t *labels, int B, int C, float c,
                                   uint16_t *dz, int lddz, float *row_loss, uint32_t *bad_labels, int threads,

@@ -184,6 +184,34 @@ __device__ __forceinline__ uint32_t mask_pair(uint32_t w, uint32_t mw)
 __device__ __forceinline__ void nonfinite_acc(uint32_t w, uint32_t &acc) { acc |= (w & 0x7C007C00u) + 0x04000400u; }
 __device__ __forceinline__ bool nonfinite_any(uint32_t acc) { return (acc & 0x80008000u) != 0; }
 
+// Factor on 32 FP32 sums before rounding; 1 (every ordinary product) costs one uniform branch.
+__device__ __forceinline__ void scale32(uint32_t (&r)[32], float alpha)
+{
+    if (alpha != 1.0f) {
+#pragma unroll
+        for (int i = 0; i < 32; i++) r[i] = __float_as_uint(__fmul_rn(__uint_as_float(r[i]), alpha));
+    }
+}
+// 32 FP32 sums plus those that earlier row blocks left at acc (16-byte aligned).
+__device__ __forceinline__ void add_acc32(uint32_t (&r)[32], const float *acc)
+{
+#pragma unroll
+    for (int v = 0; v < 8; v++) {
+        const float4 x = __ldcg((const float4 *)acc + v);
+        r[4 * v] = __float_as_uint(__fadd_rn(__uint_as_float(r[4 * v]), x.x));
+        r[4 * v + 1] = __float_as_uint(__fadd_rn(__uint_as_float(r[4 * v + 1]), x.y));
+        r[4 * v + 2] = __float_as_uint(__fadd_rn(__uint_as_float(r[4 * v + 2]), x.z));
+        r[4 * v + 3] = __float_as_uint(__fadd_rn(__uint_as_float(r[4 * v + 3]), x.w));
+    }
+}
+__device__ __forceinline__ void store_acc32(const uint32_t (&r)[32], float *acc)
+{
+#pragma unroll
+    for (int v = 0; v < 8; v++)
+        __stcg((float4 *)acc + v, make_float4(__uint_as_float(r[4 * v]), __uint_as_float(r[4 * v + 1]),
+                                              __uint_as_float(r[4 * v + 2]), __uint_as_float(r[4 * v + 3])));
+}
+
 // Epilogue of one thread for 32 consecutive accumulator columns of its output row:
 // optional ReLU on the FP32 sum, round to FP16, optional ReLU-derivative mask taken from a
 // stored FP16 activation (keep where it is > 0), inf/NaN vote, 128-bit stores where the
@@ -556,7 +584,7 @@ __device__ __forceinline__ void bulk_wait_group_read()
 // (always, so that callers can count groups).  The caller makes sure the box is free (bulk_wait_group_read).
 __device__ __forceinline__ void epilogue_box_store(uint32_t taddr, uint32_t box, const CUtensorMap *tmC, int row0, int colb,
                                                    int M, int N, bool relu, const uint16_t *mrow, bool row_ok,
-                                                   uint32_t &acc_bits)
+                                                   uint32_t &acc_bits, float alpha)
 {
     const int lane = threadIdx.x & 31;
 #pragma unroll
@@ -564,6 +592,7 @@ __device__ __forceinline__ void epilogue_box_store(uint32_t taddr, uint32_t box,
         uint32_t r[32], hw[16];
         tc_ld32(taddr + (uint32_t)(h * 32), r);
         tc_wait_ld();
+        scale32(r, alpha);
         round_pack32(r, relu, hw);
         const int col0 = colb + h * 32;
         if (mrow && row_ok) {
@@ -597,6 +626,110 @@ __device__ __forceinline__ void epilogue_box_store(uint32_t taddr, uint32_t box,
         if (row0 < M && colb < N) tma_store_2d(tmC, box, colb, row0);
         bulk_commit_group();
     }
+}
+
+// Softmax epilogue of one thread for one group of 128 classes (see CeEpi): the group's accumulators are read
+// twice from tensor memory (32 at a time), for their maximum and for the exponentials.  Per logit one FMA, one
+// ex2 on the special-function unit, one addition and half a conversion: 16 results per cycle and SM, about 2100
+// cycles for a CTA's 128 x 256 block, under a main loop of 8 k-blocks or more.  BOX: the FP16 exponentials leave
+// through the two shared-memory boxes of the warp and tensor stores (as in epilogue_box_store), otherwise by
+// 16-byte stores of the lane's own row.  V: classes (columns from V on count nothing and are written as zeros up
+// to the next multiple of 8).
+__device__ __forceinline__ float ex2_approx(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <bool BOX>
+__device__ __forceinline__ void epilogue_ce_group(uint32_t taddr, int col0, int V, int row0, int M, uint16_t *crow, const CeEpi &e,
+                                                  int label, uint32_t box_pair, const CUtensorMap *tmC, int &boxes_sent)
+{
+    constexpr float LOG2E = 1.4426950408889634f;
+    const int lane = threadIdx.x & 31, row = row0 + lane;
+    const bool row_ok = row < M;
+    float m = -INFINITY;
+#pragma unroll 1
+    for (int c = 0; c < 4; c++) {
+        uint32_t r[32];
+        tc_ld32(taddr + (uint32_t)(c * 32), r);
+        tc_wait_ld();
+        const int left = V - (col0 + c * 32);            // classes left from this chunk on
+        if (left < 32) {
+#pragma unroll
+            for (int i = 0; i < 32; i++)
+                if (i >= left) r[i] = 0xFF800000u;       // -inf
+        }
+        float m4[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            m4[i] = fmaxf(__uint_as_float(r[i]), __uint_as_float(r[i + 4]));
+#pragma unroll
+            for (int k = 8; k < 32; k += 4) m4[i] = fmaxf(m4[i], __uint_as_float(r[i + k]));
+        }
+        m = fmaxf(m, fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])));
+        if (__any_sync(0xFFFFFFFFu, (unsigned)(label - (col0 + c * 32)) < 32u)) {
+            const int at = label - (col0 + c * 32);
+            float z = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 32; i++)
+                if (i == at) z = __uint_as_float(r[i]);
+            if ((unsigned)at < 32u) e.zlabel[row] = z;
+        }
+    }
+    // a group of nothing but -inf gets the exponent of a maximum of 0: its terms are zeros, not NaN
+    const float b = m == -INFINITY ? 14.0f : fmaf(-m, LOG2E, 14.0f);
+    float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int c = 0; c < 4; c++) {
+        uint32_t r[32], w[16];
+        tc_ld32(taddr + (uint32_t)(c * 32), r);
+        tc_wait_ld();
+        const int left = V - (col0 + c * 32);
+        float x[32];
+#pragma unroll
+        for (int i = 0; i < 32; i++) x[i] = ex2_approx(fmaf(__uint_as_float(r[i]), LOG2E, b));
+        if (left < 32) {
+#pragma unroll
+            for (int i = 0; i < 32; i++)
+                if (i >= left) x[i] = 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < 32; i++) s4[i & 3] += x[i];
+        if (!e.store) continue;
+#pragma unroll
+        for (int i = 0; i < 16; i++) w[i] = pack_f16x2(x[2 * i], x[2 * i + 1]);
+        if (BOX) {
+            const uint32_t box = box_pair + (uint32_t)((boxes_sent & 1) * 4096);
+            if ((c & 1) == 0) {
+                if (lane == 0 && boxes_sent >= 2) bulk_wait_group_read<1>();     // the store before last has left this box
+                __syncwarp();
+            }
+#pragma unroll
+            for (int g8 = 0; g8 < 4; g8++) {
+                const uint32_t piece = (uint32_t)(((c & 1) * 4 + g8) ^ (lane & 7));      // 128-byte swizzle
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(box + (uint32_t)(lane * 128) + (piece << 4)),
+                             "r"(w[4 * g8]), "r"(w[4 * g8 + 1]), "r"(w[4 * g8 + 2]), "r"(w[4 * g8 + 3])
+                             : "memory");
+            }
+            if (c & 1) {
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // the tensor store reads what the lanes wrote
+                __syncwarp();
+                if (lane == 0) {
+                    const int colb = col0 + (c - 1) * 32;
+                    if (row0 < M && colb < V) tma_store_2d(tmC, box, colb, row0);
+                    bulk_commit_group();
+                }
+                boxes_sent++;
+            }
+        } else if (row_ok) {
+#pragma unroll
+            for (int g8 = 0; g8 < 4; g8++)
+                if (g8 * 8 < left)
+                    *(uint4 *)(crow + col0 + c * 32 + g8 * 8) = make_uint4(w[4 * g8], w[4 * g8 + 1], w[4 * g8 + 2], w[4 * g8 + 3]);
+        }
+    }
+    if (row_ok && col0 < V) e.stats[(size_t)(col0 >> 7) * M + row] = make_float2((s4[0] + s4[1]) + (s4[2] + s4[3]), b);
 }
 
 // The same load with an L2 eviction-priority hint (policy from l2_policy()).  Operand lines marked
