@@ -570,6 +570,30 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
                   float *loss_dev, uint32_t *bad_labels_dev, uint32_t *nonfinite_flag_dev, uint32_t *status_dev,
                   void *workspace_dev, size_t workspace_bytes, void *cuda_stream);
 
+/* Distillation from a teacher's top logits (sections 3.2, 3.3: FP32 softmax arithmetic on FP16 logits, gradient
+ * scaled before it is rounded; the paper has no teacher).  Row r has K entries (idx[r,j], t[r,j]): classes and the
+ * teacher's logits for them.  With temperature tau:
+ *   q = softmax over the row's entries of t / tau        p = softmax over all C classes of z / tau
+ *   row_loss[r] = tau^2 * sum_j q_j * (log q_j - log p[idx_j])       loss = mean over the B rows
+ *   dz[r,v]     = rn16(tau * (p[v] - sum of q_j with idx_j = v) * S / B)
+ * An entry whose class is outside [0, C), or whose logit is -inf, has no part in it (lists of different lengths are
+ * padded with class -1); a row without any entry left contributes neither loss nor gradient (its row of dz is zero;
+ * the mean still divides by B).  A class named more than once counts with the sum of its probabilities.  NaN in a
+ * row of z or among its entries' logits makes that row's loss NaN.
+ * z, dz: FP16 [B, C] with pitches in elements; t16: FP16 and idx: int32, both [B, K] with pitch ldt.  dz_dev may be
+ * null (losses only; lddz is then ignored).  To mix with a hard label, call mpt_softmax_ce with the other share of S
+ * and add the two gradients (mpt_add_f16).
+ * status_dev (may be null): one uint32 the caller has zeroed, receives a time-out code if a bounded wait runs out
+ * (results are then invalid).  z and dz must not overlap.  Any B >= 0, 1 <= C <= MPT_DISTILL_MAX_C, 1 <= K <=
+ * MPT_DISTILL_MAX_K; tau > 0; rows that are 16-byte aligned move by bulk copies, others element by element.
+ * Nothing is allocated and no workspace is needed.  Results are run-to-run identical.  Asynchronous on the stream,
+ * which must belong to the current device.  Bytes moved per logit: 4. */
+#define MPT_DISTILL_MAX_K 1024
+#define MPT_DISTILL_MAX_C (1 << 26)
+int mpt_distill_topk(const uint16_t *z_dev, int ldz, int B, int C, const uint16_t *t16_dev, const int32_t *idx_dev, int ldt, int K,
+                     float tau, float S, uint16_t *dz_dev, int lddz, float *row_loss_dev, float *loss_dev, uint32_t *status_dev,
+                     void *cuda_stream);
+
 /* mpt_softmax_ce without the caller-provided scratch.  (The paper has no counterpart:
  * this entry point exists for the sake of callers, not of the method.)
  *

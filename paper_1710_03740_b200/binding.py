@@ -40,7 +40,7 @@ EXPORTS = ["mpt_workspace_bytes", "mpt_create", "mpt_workspace_bytes_opt", "mpt_
            "mpt_lstm_forward", "mpt_lstm_backward", "mpt_lstm_cell_forward", "mpt_lstm_cell_backward", "mpt_bias_grad",
            "mpt_add_f16",
            "mpt_layernorm_forward", "mpt_layernorm_workspace_bytes", "mpt_layernorm_backward",
-           "mpt_linear_ce_workspace_bytes", "mpt_linear_ce",
+           "mpt_linear_ce_workspace_bytes", "mpt_linear_ce", "mpt_distill_topk",
            "mpt_dp_shard", "mpt_dp_step_flat", "mpt_dp_alloc", "mpt_dp_free", "mpt_dp_export", "mpt_dp_open", "mpt_dp_close",
            "mpt_dp_layout_of", "mpt_dp_attach", "mpt_dp_step_flat_opt", "mpt_dp_norm_flat", "mpt_dp_norm",
            "mpt_workspace_bytes_dp", "mpt_create_dp", "mpt_state_range", "mpt_dp_overlap_events", "mpt_dp_overlap_attach",
@@ -163,6 +163,7 @@ def lib() -> C.CDLL:
     L.mpt_layernorm_backward.argtypes = [i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
     L.mpt_linear_ce_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, C.POINTER(sz)]
     L.mpt_linear_ce.argtypes = [i32, i32, i32, vp, i32, vp, i32, vp, f32, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.mpt_distill_topk.argtypes = [vp, i32, i32, i32, vp, vp, i32, i32, f32, f32, vp, i32, vp, vp, vp, vp]
     L.mpt_dp_shard.argtypes = [sz, i32, i32, C.POINTER(sz), C.POINTER(sz)]
     L.mpt_dp_step_flat.argtypes = [vp, vp, vp, vp, vp, sz, i32, i32, f32, f32, f32, vp, vp]
     L.mpt_dp_step_flat_opt.argtypes = [C.POINTER(Optimizer), vp, vp, vp, vp, vp, vp, sz, i32, i32, f32, f32, f32, vp, vp, vp, vp]
@@ -599,6 +600,13 @@ def mpt_linear_ce(N, V, H, x, ldx, W, ldw, labels, S, row_loss, loss, dx, lddx, 
     _check(lib().mpt_linear_ce(N, V, H, _at(x), ldx, _at(W), ldw, _at(labels), S, row_block, _at(dx), lddx, _at(dW), lddw,
                                _at(row_loss), _at(loss), _at(bad_labels), _at(nonfinite_flag), _at(status), _at(workspace),
                                workspace.numel(), st))
+
+
+def mpt_distill_topk(z, ldz, B, Cn, t16, idx, ldt, K, tau, S, dz, lddz, row_loss, loss, status=None, stream=None):
+    """dz may be None (losses only)."""
+    st = _stream_of(stream, ((z, 2), (t16, 2), (idx, 4), (dz, 2), (row_loss, 4), (loss, 4), (status, 4)))
+    _check(lib().mpt_distill_topk(_at(z), ldz, B, Cn, _at(t16), _at(idx), ldt, K, tau, S, _at(dz), lddz, _at(row_loss), _at(loss),
+                                  _at(status), st))
 
 
 class LstmLayer:
