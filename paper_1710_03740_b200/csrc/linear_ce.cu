@@ -9,7 +9,7 @@
 // writing dW).  The rows go through in blocks of R; per block
 //   1  the logits product with a softmax epilogue: the accumulators of 128 classes of a row become FP16
 //      exponentials relative to their own maximum (CeEpi), with their FP32 sum, and the label's FP32 logit
-//   2  k_ce_combine: log2 of the row's whole sum, and the row's loss (and x without the ignored rows, for step 5)
+//   2  k_ce_combine: the row's whole sum, and the row's loss (and x without the ignored rows, for step 5)
 //   3  k_ce_rescale: exponentials -> 2^14 (p - [v = y]) in place
 //   4  dx = product of those with W, 5 dW = product of their transpose with x, both with the factor S / N * 2^-14
 //      in the epilogue
@@ -25,6 +25,7 @@ namespace mpt {
 namespace {
 
 constexpr int kGroup = 128;           // classes of one softmax group (CeEpi)
+constexpr float kLog2e = 1.4426950408889634f;      // as in the softmax epilogue
 constexpr int kDefaultRows = 4096;    // rows of a block when the caller does not choose
 
 __device__ __forceinline__ float ex2(float x)
@@ -34,13 +35,14 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-// Row sums from the group sums: lse2 = log2 sum_g s_g 2^(-b_g), and the row's loss.  Four rows per CTA (a 32-byte
+// Row sums from the group sums: sum_g s_g 2^(-b_g) = y 2^x as the pair (x, y), x the largest -b_g, and the row's
+// loss.  The pair stays apart: log2 of large logits' sum as one FP32 number would not resolve p.  Four rows per CTA (a 32-byte
 // sector of `stats` holds one group of four rows), 64 threads a row; fixed order.
 // xs (null: not wanted) receives x with the rows of ignored labels as zeros: what a padding row holds, NaN
 // perhaps, must not meet its zero gradient in dW's product.
 __global__ void __launch_bounds__(256) k_ce_combine(const float2 *__restrict__ stats, int R, int V, int groups,
                                                     const int32_t *__restrict__ labels, const float *__restrict__ zlabel,
-                                                    float *__restrict__ lse2, float *__restrict__ row_loss, uint32_t *bad_labels,
+                                                    float2 *__restrict__ rowsum, float *__restrict__ row_loss, uint32_t *bad_labels,
                                                     const uint16_t *__restrict__ x, int ldx, int H, uint16_t *__restrict__ xs)
 {
     pdl_trigger();
@@ -85,8 +87,9 @@ __global__ void __launch_bounds__(256) k_ce_combine(const float2 *__restrict__ s
         for (int w = 1; w < 8; w++) join(m, s, red[w][r].x, red[w][r].y);
         const int y = labels[row];
         const bool good = y >= 0 && y < V;
-        lse2[row] = m + log2f(s);
-        if (good) row_loss[row] = (float)(((double)m + log2((double)s)) * 0.69314718055994530942 - (double)zlabel[row]);
+        rowsum[row] = make_float2(m, s);
+        // the label's logit in the same units as the reference, so that what log2(e) loses as an FP32 number cancels
+        if (good) row_loss[row] = (float)(((double)m - (double)zlabel[row] * (double)kLog2e + log2((double)s)) * 0.69314718055994530942);
         else row_loss[row] = 0.0f;                      // contributes neither loss nor gradient
         if (!good && bad_labels) atomicAdd(bad_labels, 1u);
     }
@@ -96,7 +99,7 @@ __global__ void __launch_bounds__(256) k_ce_combine(const float2 *__restrict__ s
 // first use; the eight warps of a CTA take neighbouring rows, which share the sectors of `stats`.
 __global__ void __launch_bounds__(256) k_ce_rescale(uint16_t *__restrict__ e16, int ld, const float2 *__restrict__ stats, int R,
                                                     int V, const int32_t *__restrict__ labels, const float *__restrict__ zlabel,
-                                                    const float *__restrict__ lse2)
+                                                    const float2 *__restrict__ rowsum)
 {
     pdl_trigger();
     pdl_wait();
@@ -108,7 +111,8 @@ __global__ void __launch_bounds__(256) k_ce_rescale(uint16_t *__restrict__ e16, 
     const bool good = y >= 0 && y < V;
     uint4 v[8];
     float f[8];
-    const float lse = lse2[row];
+    const float2 sum = rowsum[row];
+    const float inv = __fdiv_rn(1.0f, sum.y);
 #pragma unroll
     for (int u = 0; u < 8; u++) {
         const int col = col0 + u * 256;
@@ -124,7 +128,7 @@ __global__ void __launch_bounds__(256) k_ce_rescale(uint16_t *__restrict__ e16, 
         uint32_t w[4] = {0u, 0u, 0u, 0u};
         if (good) {
             const uint32_t x[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-            const float k = ex2((14.0f - f[u]) - lse);
+            const float k = ex2((-f[u] - sum.x) + 14.0f) * inv;
 #pragma unroll
             for (int q = 0; q < 4; q++) {
                 const float2 t = __half22float2(*(const __half2 *)&x[q]);
@@ -132,7 +136,7 @@ __global__ void __launch_bounds__(256) k_ce_rescale(uint16_t *__restrict__ e16, 
                 w[q] = *(const uint32_t *)&h;
             }
             if (y - col >= 0 && y - col < 8) {           // the label's element from its FP32 logit
-                const float p = ex2(fmaf(zlabel[row], 1.4426950408889634f, -lse));
+                const float p = ex2(fmaf(zlabel[row], kLog2e, -sum.x)) * inv;
                 const uint32_t h = (uint32_t)__half_as_ushort(__float2half_rn((p - 1.0f) * 16384.0f));
 #pragma unroll
                 for (int q = 0; q < 4; q++) {
@@ -150,7 +154,7 @@ struct Plan {
     int lde;              // pitch of the exponentials
     int groups;
     int ldacc;
-    size_t e16, stats, lse2, zlabel, xs, splitk, splitk_bytes, acc32, total;
+    size_t e16, stats, rowsum, zlabel, xs, splitk, splitk_bytes, acc32, total;
 };
 
 // The split of dx's contraction over the vocabulary: for few rows the product has few tiles and reading W is what
@@ -182,7 +186,7 @@ Plan make_plan(int N, int V, int H, bool want_dx, bool want_dW, int row_block)
     const bool grads = want_dx || want_dW;
     p.e16 = take(grads ? (size_t)p.R * p.lde * 2 : 0);
     p.stats = take((size_t)p.groups * p.R * sizeof(float2));
-    p.lse2 = take((size_t)p.R * sizeof(float));
+    p.rowsum = take((size_t)p.R * sizeof(float2));
     p.zlabel = take((size_t)p.R * sizeof(float));
     p.xs = take(want_dW ? (size_t)p.R * H * 2 : 0);
     size_t sk = 0;
@@ -257,7 +261,8 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
     uint8_t *ws = (uint8_t *)workspace_dev;
     uint16_t *e16 = (uint16_t *)(ws + p.e16);
     float2 *stats = (float2 *)(ws + p.stats);
-    float *lse2 = (float *)(ws + p.lse2), *zlabel = (float *)(ws + p.zlabel);
+    float2 *rowsum = (float2 *)(ws + p.rowsum);
+    float *zlabel = (float *)(ws + p.zlabel);
     uint16_t *xs = dW_dev ? (uint16_t *)(ws + p.xs) : nullptr;
     const bool grads = dx_dev || dW_dev;
     cudaError_t e = cudaSuccess;
@@ -274,10 +279,10 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
         e = product(MPT_OP_FWD, R, V, H, x, ldx, W_dev, ldw, grads ? e16 : nullptr, p.lde, xl, nullptr, status_dev, nullptr, 0, st);
         if (e != cudaSuccess) break;
         e = launch_pdl(k_ce_combine, dim3((unsigned)((R + 3) / 4)), dim3(256), 0, st, (const float2 *)stats, R, V, p.groups, labels,
-                       (const float *)zlabel, lse2, row_loss_dev + r0, bad_labels_dev, x, ldx, H, xs);
+                       (const float *)zlabel, rowsum, row_loss_dev + r0, bad_labels_dev, x, ldx, H, xs);
         if (e != cudaSuccess || !grads) continue;
         e = launch_pdl(k_ce_rescale, dim3((unsigned)((p.lde + 2047) / 2048), (unsigned)((R + 7) / 8)), dim3(256), 0, st, e16, p.lde,
-                       (const float2 *)stats, R, V, labels, (const float *)zlabel, (const float *)lse2);
+                       (const float2 *)stats, R, V, labels, (const float *)zlabel, (const float2 *)rowsum);
         if (e == cudaSuccess && dx_dev) {
             xd.alpha = alpha;
             xd.max_split = kDxSplit;

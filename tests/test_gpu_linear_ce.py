@@ -174,6 +174,32 @@ def test_peaked_flat_and_tiny_probabilities(N, V):
         check(x, W, y, S, call(x, W, y, S))
 
 
+def test_large_logits():
+    """Logits of several thousand: the exponents' reference and the sum relative to it stay apart, so p is as exact as the
+    logits are.  Integer operands make every logit exact, so that the bound on d is the roundings' alone."""
+    N, V, H = 24, 700, 64
+    rng = np.random.default_rng(4)
+    x = rng.integers(-8, 9, (N, H)).astype(np.float16) * 4
+    W = rng.integers(-8, 9, (V, H)).astype(np.float16)
+    x[:, :2] = 128.0
+    W[:, 0] = 60.0                            # every logit is raised by 7680
+    W[:, 1] = rng.integers(-3, 4, V) / 64.0
+    W[:, 2:] = 0                              # what is left differs by steps of 2
+    y = rng.integers(0, V, N).astype(np.int32)
+    got = call(x, W, y, 64.0)
+    z = x.astype(np.float64) @ W.astype(np.float64).T
+    p = np.exp(z - z.max(1, keepdims=True))
+    p /= p.sum(1, keepdims=True)
+    d = p.copy()
+    d[np.arange(N), y] -= 1
+    # the exponents' rounding: |z log2 e| up to 2^14, rounded to 2^-10 / 2 of an exponent, but the same for one reference;
+    # differences of logits are exact multiples of 2, so only the reference's own 24 bits count: (2^-10) ln 2 in the worst case
+    err = np.abs(d) * 2 * H16 + p * 2.0 ** -10
+    ref = (64.0 / N) * (d @ W.astype(np.float64))
+    tol = (64.0 / N) * ((err + 2.0 ** -38) @ np.abs(W.astype(np.float64)) + (tc(V) + 4 * U) * (np.abs(d) @ np.abs(W.astype(np.float64))))
+    assert np.all(np.abs(got["dx"].cpu().numpy() - ref) <= tol + H16 * (np.abs(ref) + tol) + 2.0 ** -25)
+
+
 def test_nonfinite_values_reach_what_they_must():
     x, W, y = make(40, 500, 64, 23)
     x[5, 1] = np.nan
