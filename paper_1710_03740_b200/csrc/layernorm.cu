@@ -107,8 +107,10 @@ struct LnFwd {
 };
 
 // One row per warp (WARP) or per CTA; thread t of the group holds the vectors t, t + T, ... (at most VPT).
-template <int VPT, bool VEC, bool WARP>
-__global__ void __launch_bounds__(WARP ? 256 : 1024) k_ln_fwd(const LnFwd p)
+// MAXT threads at most; rows of one CTA are kept to 384 threads where they fit (12288 features), so that four
+// CTAs share an SM and one row's loads run under another's reductions.
+template <int VPT, bool VEC, bool WARP, int MAXT>
+__global__ void __launch_bounds__(MAXT, MAXT == 384 ? 4 : 1) k_ln_fwd(const LnFwd p)
 {
     pdl_trigger();
     pdl_wait();
@@ -138,10 +140,18 @@ __global__ void __launch_bounds__(WARP ? 256 : 1024) k_ln_fwd(const LnFwd p)
             const int col = (t + u * T) * 8;
             float f[8];
             unpack8(v[u], f);
+            if (col + 8 <= p.cols) {
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const float d = f[e] - mean;
-                if (col + e < p.cols) d2 = fmaf(d, d, d2);
+                for (int e = 0; e < 8; e++) {
+                    const float d = f[e] - mean;
+                    d2 = fmaf(d, d, d2);
+                }
+            } else if (col < p.cols) {
+#pragma unroll
+                for (int e = 0; e < 7; e++) {
+                    const float d = f[e] - mean;
+                    if (col + e < p.cols) d2 = fmaf(d, d, d2);
+                }
             }
         }
         const float var = __fdiv_rn(WARP ? warp_sum(d2) : cta_sum(d2, red[1]), n);
@@ -458,11 +468,11 @@ constexpr int kLnMaxCols = 1 << 30;   // column indexes stay far inside 32 bits
 int ln_colp(int cols) { return (cols + 7) / 8 * 8; }
 int ln_parts(int rows) { return rows < kLnMaxParts ? rows : kLnMaxParts; }
 
-template <int VPT, bool WARP>
+template <int VPT, bool WARP, int MAXT>
 cudaError_t run_fwd(const LnFwd &p, bool vec, int grid, int threads, cudaStream_t st)
 {
-    if (vec) MPT_LAUNCH((k_ln_fwd<VPT, true, WARP>), dim3((unsigned)grid), dim3((unsigned)threads), 0, st, p);
-    else MPT_LAUNCH((k_ln_fwd<VPT, false, WARP>), dim3((unsigned)grid), dim3((unsigned)threads), 0, st, p);
+    if (vec) MPT_LAUNCH((k_ln_fwd<VPT, true, WARP, MAXT>), dim3((unsigned)grid), dim3((unsigned)threads), 0, st, p);
+    else MPT_LAUNCH((k_ln_fwd<VPT, false, WARP, MAXT>), dim3((unsigned)grid), dim3((unsigned)threads), 0, st, p);
     return cudaSuccess;
 }
 
@@ -486,16 +496,15 @@ cudaError_t launch_ln_fwd(const LnFwd &p, cudaStream_t st)
         warps = warps < 1 ? 1 : (warps > 8 ? 8 : warps);
         const long ctas = ((long)p.rows + warps - 1) / warps;
         const int grid = (int)(ctas < 148 * 8 ? ctas : 148 * 8);
-        if (c8 <= 32) return run_fwd<1, true>(p, vec, grid, warps * 32, st);
-        if (c8 <= 64) return run_fwd<2, true>(p, vec, grid, warps * 32, st);
-        return run_fwd<4, true>(p, vec, grid, warps * 32, st);
+        if (c8 <= 32) return run_fwd<1, true, 256>(p, vec, grid, warps * 32, st);
+        if (c8 <= 64) return run_fwd<2, true, 256>(p, vec, grid, warps * 32, st);
+        return run_fwd<4, true, 256>(p, vec, grid, warps * 32, st);
     }
     if (c8 <= 4 * 1024) {
-        const int vpt = c8 <= 2048 ? 2 : 4;
-        const int threads = ((c8 + vpt - 1) / vpt + 31) / 32 * 32;
-        const int per_sm = 2048 / threads;
+        const int threads = ((c8 + 3) / 4 + 31) / 32 * 32;
+        const int per_sm = threads <= 384 ? (1536 / threads < 16 ? 1536 / threads : 16) : 1;
         const int grid = p.rows < 148 * per_sm ? p.rows : 148 * per_sm;
-        return vpt == 2 ? run_fwd<2, false>(p, vec, grid, threads, st) : run_fwd<4, false>(p, vec, grid, threads, st);
+        return threads <= 384 ? run_fwd<4, false, 384>(p, vec, grid, threads, st) : run_fwd<4, false, 1024>(p, vec, grid, threads, st);
     }
     const int grid = p.rows < 296 ? p.rows : 296;
     if (vec) MPT_LAUNCH(k_ln_fwd_long<true>, dim3((unsigned)grid), dim3(1024), 0, st, p);
