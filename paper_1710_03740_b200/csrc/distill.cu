@@ -4,17 +4,16 @@
 //   q = softmax over the row's entries of t / tau ;  p = softmax over all C classes of z / tau
 //   loss = tau^2 sum_j q_j (log q_j - log p_c(j)) ;  dz_v = rn16(tau * (p_v - sum of q_j with c(j) = v) * S / B)
 //
-// Bound: HBM, 4 bytes a logit (z read once, dz written once).  A row is spread over the warps of one CTA or of a
-// cluster of 2, 4 or 8, so that its logits stay in shared memory between the two passes over them.  Every warp is a
-// pipeline of its own over its part of every row: bulk copies in, running maximum and sum of exponentials, bulk copy
-// out of the gradient formed in place.  The only thing warps exchange is one (reference, sum) pair per row, through
-// distributed shared memory and one cluster barrier, whose two halves have the first pass over the NEXT row between
-// them; so nothing waits for the slowest warp, and loads and stores are always in flight.  One more warp per CTA
-// prepares the teacher's entries while the others work.
-// Exponentials are taken twice (once per pass) rather than kept: 2.1 special-function results a logit are 4300
-// cycles for 32000 logits of a row, against 5600 cycles that its 128 KB take at an SM's share of HBM.
-// Rows too long for the shared memory of 8 CTAs (about 430 000 classes) are read a second time instead, from L2: the
-// rows in work at any moment are a few tens of MB.
+// Bound: HBM, 4 bytes a logit (z read once, dz written once).  A row is spread over up to 16 warps of a CTA or over a
+// cluster of 2, 4 or 8 CTAs.  Every warp is a pipeline of its own over its part of every row: bulk copies in ahead of
+// time, sum of exponentials, gradient out.  What warps exchange is one (reference, sum)
+// pair per row, through (distributed) shared memory and an mbarrier; two more warps per CTA prepare the teacher's
+// entries rows ahead.
+//   Up to 32768 logits per CTA (262144 per row) the exponentials stay in registers between the two uses, each lane's
+// relative to its own maximum: one special-function result and about 6 instructions a logit.
+//   Longer rows pass through shared memory twice, the second time from L2 (clusters of 4: about 33 rows of 1.6 MB are
+// in work at a time; first reads are marked to stay, second reads and the gradient to leave first), and take their
+// exponentials twice.
 #include <math.h>
 
 #include "mpt_common.cuh"
@@ -38,20 +37,33 @@ struct DistillArgs {
     size_t lddz;
     float *row_loss;
     uint32_t *kerr;
-    int nw;              // warps that hold logits (one more prepares the teacher's entries)
+    int nw;              // warps that hold logits (kTeachers more prepare the teacher's entries)
     int wv;              // vectors of 8 logits per warp
     int vp;              // vectors per CTA
     int cl;              // CTAs per cluster
     int ns;              // buffers per warp
-    int chunk;           // streamed rows: vectors per buffer
+    int nb_log2;         // buffers for a row's entries: 2^nb_log2
+    int per;             // vectors per buffer: wv, or a chunk of it where rows are streamed
 };
 
-struct Entry {
-    int32_t v;           // class, -1: none
-    float q;             // teacher's probability
-    float z;             // student's logit
+// A row's teacher entries in shared memory, each array K long: class (-1: none), teacher's probability, the student's
+// logit (kept by the warp that holds it while the gradient takes its place), and the teacher's probability of the class
+// (q, or of all entries that name it).
+// The entries of the classes that warp w of this CTA holds are order[first[w]] ... order[first[w + 1] - 1].
+struct Entries {
+    int32_t *v;
+    float *q, *z, *sum;
+    int32_t *order, *first;
 };
-constexpr int kEntryBuffers = 3;
+constexpr int kEntryWords = 5;       // 32-bit words an entry takes
+constexpr int kPairBuffers = 4;      // a warp publishes row i + 1 when all have finished with row i - 3
+constexpr int kNoClass = -1;
+constexpr int kTeachers = 2;         // warps that prepare the teacher's entries, every kTeachers-th row each
+constexpr unsigned kNap = 64;        // ns
+constexpr int kAhead = 4;            // rows of its own a teacher warp asks for ahead
+constexpr int kMaxWarps = 16;        // warps that hold logits: few, so that what each does once per row stays small
+constexpr int kMaxRounds = 8;        // vectors a lane keeps in registers
+constexpr int kChunk = 256;          // vectors of a buffer where rows are streamed
 constexpr uint32_t kNegInf16 = 0xFC00u;
 
 __device__ __forceinline__ float h2f(uint32_t h) { return __half2float(__ushort_as_half((unsigned short)h)); }
@@ -62,11 +74,11 @@ __device__ __forceinline__ float wsum(float v)
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     return v;
 }
-__device__ __forceinline__ float wmax(float v)
+__device__ __forceinline__ float wmax(float v)      // NaN operands are dropped, as by fmaxf
 {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-    return v;
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
 }
 
 // Running sum of a lane: sum of 2^(z k + b) with b = -max * k as it was rounded, so the pair says exactly what
@@ -74,9 +86,17 @@ __device__ __forceinline__ float wmax(float v)
 struct Run {
     float m = -INFINITY, b = 0.0f, s = 0.0f;
 };
-__device__ __forceinline__ void run_add8(Run &r, const uint4 x, float k)
+__device__ __forceinline__ __half2 max8(const uint4 x)
 {
-    const __half2 mx = __hmax2(__hmax2(*(const __half2 *)&x.x, *(const __half2 *)&x.y), __hmax2(*(const __half2 *)&x.z, *(const __half2 *)&x.w));
+    return __hmax2(__hmax2(*(const __half2 *)&x.x, *(const __half2 *)&x.y), __hmax2(*(const __half2 *)&x.z, *(const __half2 *)&x.w));
+}
+// N vectors at once: one comparison with the running maximum for all of them.
+template <int N>
+__device__ __forceinline__ void run_add(Run &r, const uint4 (&x)[N], float k)
+{
+    __half2 mx = max8(x[0]);
+#pragma unroll
+    for (int u = 1; u < N; u++) mx = __hmax2(mx, max8(x[u]));
     const float m = fmaxf(__low2float(mx), __high2float(mx));       // NaN is dropped here and comes back in the sum
     if (m > r.m) {
         const float b = -__fmul_rn(m, k);
@@ -84,21 +104,46 @@ __device__ __forceinline__ void run_add8(Run &r, const uint4 x, float k)
         r.m = m;
         r.b = b;
     }
-    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-    float a[4];
+    float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int q = 0; q < 4; q++) {
-        const float2 f = __half22float2(*(const __half2 *)&w[q]);
-        a[q] = ex2_approx(fmaf(f.x, k, r.b)) + ex2_approx(fmaf(f.y, k, r.b));
+    for (int u = 0; u < N; u++) {
+        const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            const float2 f = __half22float2(*(const __half2 *)&w[q]);
+            a[q] += ex2_approx(fmaf(f.x, k, r.b));
+            a[q] += ex2_approx(fmaf(f.y, k, r.b));
+        }
     }
     r.s += (a[0] + a[1]) + (a[2] + a[3]);
 }
-// The warp's pair: reference e (terms are relative to 2^e), sum.  A lane with e = -inf has nothing or NaN to add.
-__device__ __forceinline__ float2 run_warp(const Run &r)
+// n vectors of shared memory, lane by lane; the warp's rounds of 32 go four at a time
+__device__ __forceinline__ void run_vectors(Run &r, const uint4 *v, int n, float k)
 {
-    const float e = r.m == -INFINITY ? -INFINITY : -r.b;
+    const int lane = threadIdx.x & 31;
+    int base = 0;
+    for (; base + 128 <= n; base += 128) {
+        const uint4 *s = v + base + lane;
+        const uint4 x[4] = {s[0], s[32], s[64], s[96]};
+        run_add<4>(r, x, k);
+    }
+    if (base + 64 <= n) {
+        const uint4 *s = v + base + lane;
+        const uint4 x[2] = {s[0], s[32]};
+        run_add<2>(r, x, k);
+        base += 64;
+    }
+    for (int j = base + lane; j < n; j += 32) {
+        const uint4 x[1] = {v[j]};
+        run_add<1>(r, x, k);
+    }
+}
+// The warp's pair from its lanes': reference e (terms are relative to 2^e), sum.  A lane with e = -inf has nothing or NaN
+// to add.
+__device__ __forceinline__ float2 warp_pair(float e, float s)
+{
     const float E = wmax(e);
-    return make_float2(E, wsum(e == -INFINITY ? r.s : r.s * ex2_approx(e - E)));
+    return make_float2(E, wsum(e == -INFINITY ? s : s * ex2_approx(e - E)));
 }
 // The row's pair from those of all warps (every lane gets the same bits): p = 2^(z k - x) / y.  The two stay apart:
 // with logits near FP16's largest their log2 would be a number of 10^5, known to a hundredth only.
@@ -116,200 +161,321 @@ __device__ __forceinline__ float2 row_pair(const float2 *red, int pairs)
     return make_float2(E, wsum(s));
 }
 
-// Gradient of n vectors in place.
-__device__ __forceinline__ void grad_vectors(uint4 *v, int n, float k, float2 pr, float c, bool live)
+// Eight neighbouring gradients of a row to global memory, the first at class `first`.
+template <bool WHOLE>
+__device__ __forceinline__ void store8(uint16_t *dst, const uint4 v, int first, int C)
 {
-    const int lane = threadIdx.x & 31;
-    const float cs = __fdiv_rn(c, pr.y);
-#pragma unroll 4
-    for (int i = lane; i < n; i += 32) {
-        const uint4 x = v[i];
-        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+    if (WHOLE && first + 8 <= C) {
+        __stcs((uint4 *)dst, v);
+        return;
+    }
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        if (first + e < C) dst[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+}
+// Gradient of n vectors, 2^(z k - x) * cs with cs = tau S / (B y), from shared memory to dst (class `first` on).
+template <int N, bool WHOLE>
+__device__ __forceinline__ void grad_store(const uint4 *v, uint16_t *dst, int first, int C, float k, float x, float cs)
+{
+    uint4 in[N];
+#pragma unroll
+    for (int u = 0; u < N; u++) in[u] = v[32 * u];
+#pragma unroll
+    for (int u = 0; u < N; u++) {
+        const uint32_t w[4] = {in[u].x, in[u].y, in[u].z, in[u].w};
         uint32_t o[4];
 #pragma unroll
         for (int q = 0; q < 4; q++) {
             const float2 f = __half22float2(*(const __half2 *)&w[q]);
-            o[q] = live ? pack_f16x2(ex2_approx(fmaf(f.x, k, -pr.x)) * cs, ex2_approx(fmaf(f.y, k, -pr.x)) * cs) : 0u;
+            o[q] = pack_f16x2(ex2_approx(fmaf(f.x, k, -x)) * cs, ex2_approx(fmaf(f.y, k, -x)) * cs);
         }
-        v[i] = make_uint4(o[0], o[1], o[2], o[3]);
+        store8<WHOLE>(dst + 256 * u, make_uint4(o[0], o[1], o[2], o[3]), first + 256 * u, C);
     }
 }
-// The teacher's classes among the logits [first, first + count) that this warp holds at h: their gradient again
-// with the probabilities of all entries of that class subtracted (an entry named twice is written twice, alike).
-__device__ __forceinline__ void patch_targets(uint16_t *h, int first, int count, const Entry *ent, int K, float k, float2 pr, float c)
+template <bool WHOLE>
+__device__ __forceinline__ void grad_vectors(const uint4 *v, int n, uint16_t *dst, int first, int C, float k, float2 pr, float cs)
 {
     const int lane = threadIdx.x & 31;
-    for (int j0 = 0; j0 < K; j0 += 32) {
-        const int j = j0 + lane;
-        const int v = j < K ? ent[j].v : -1;
-        unsigned hit = __ballot_sync(0xFFFFFFFFu, v >= 0 && (unsigned)(v - first) < (unsigned)count);
-        while (hit) {
-            const int src = __ffs((int)hit) - 1;
-            hit &= hit - 1;
-            const int at = __shfl_sync(0xFFFFFFFFu, v, src);
-            float q = 0.0f;
-            for (int i = lane; i < K; i += 32)
-                if (ent[i].v == at) q += ent[i].q;
-            q = wsum(q);
-            if (lane == src) h[at - first] = (uint16_t)f2h((__fdiv_rn(ex2_approx(fmaf(ent[j].z, k, -pr.x)), pr.y) - q) * c);
-        }
+    int base = 0;
+    for (; base + 128 <= n; base += 128) grad_store<4, WHOLE>(v + base + lane, dst + (base + lane) * 8, first + (base + lane) * 8, C, k, pr.x, cs);
+    if (base + 64 <= n) {
+        grad_store<2, WHOLE>(v + base + lane, dst + (base + lane) * 8, first + (base + lane) * 8, C, k, pr.x, cs);
+        base += 64;
+    }
+    for (int j = base + lane; j < n; j += 32) grad_store<1, WHOLE>(v + j, dst + j * 8, first + j * 8, C, k, pr.x, cs);
+}
+// The teacher's classes among the logits [first, first + count) that warp w holds at h: keep their logits ...
+__device__ __forceinline__ void keep_targets(const uint16_t *h, int first, int count, const Entries &ent, int w)
+{
+    for (int j = ent.first[w] + (int)(threadIdx.x & 31); j < ent.first[w + 1]; j += 32) {
+        const int i = ent.order[j], at = ent.v[i] - first;
+        if ((unsigned)at < (unsigned)count) ent.z[i] = h2f(h[at]);
+    }
+}
+// ... and, when the warp has written the gradients of these classes at dst, write theirs again with the teacher's
+// probability of the class subtracted (an entry named twice is written twice, alike).
+__device__ __forceinline__ void patch_targets(uint16_t *dst, int first, int count, const Entries &ent, int w, float k, float2 pr, float cs, float c)
+{
+    for (int j = ent.first[w] + (int)(threadIdx.x & 31); j < ent.first[w + 1]; j += 32) {
+        const int i = ent.order[j], at = ent.v[i] - first;
+        if ((unsigned)at < (unsigned)count)
+            dst[at] = (uint16_t)f2h(fmaf(ex2_approx(fmaf(ent.z[i], k, -pr.x)), cs, -ent.sum[i] * c));
     }
 }
 
 // Teacher's entries of a row, by one warp.  Entries whose class is outside [0, C) or whose logit is -inf have no part;
-// *live: whether any has.
-__device__ __forceinline__ void prepare_entries(const DistillArgs &p, int row, Entry *ent, int *live)
+// returns whether any has.  `rank`: which CTA of the cluster this is.  Classes named more than once are found with a hash table (open addressing, `slots` words, a
+// power of two and at least 2 K); only theirs are added up, over the entries in order.
+__device__ __forceinline__ bool prepare_entries(const DistillArgs &p, int row, int rank, const Entries &ent, int *table, int slots)
 {
     const int lane = threadIdx.x & 31;
     const int32_t *id = p.idx + (size_t)row * p.ldt;
-    const uint16_t *tt = p.t + (size_t)row * p.ldt, *zr = p.z + (size_t)row * p.ldz;
+    const uint16_t *tt = p.t + (size_t)row * p.ldt;
+    for (int i = lane; i < slots; i += 32) table[i] = kNoClass;
+    if (lane < kMaxWarps) ent.first[lane] = 0;
     float top = -INFINITY;
     bool any = false;
+    __syncwarp();
 #pragma unroll 4
     for (int j = lane; j < p.K; j += 32) {
         const int v = id[j];
         const float t = h2f(tt[j]);
         const bool ok = v >= 0 && v < p.C && t != -INFINITY;
-        Entry e;
-        e.v = ok ? v : -1;
-        e.q = t;
-        e.z = ok ? h2f(zr[v]) : 0.0f;
-        ent[j] = e;
+        ent.v[j] = ok ? v : kNoClass;
+        ent.q[j] = t;
         if (ok) top = fmaxf(top, t);
         any |= ok;
     }
     top = wmax(top);
-    any = __any_sync(0xFFFFFFFFu, any);
     float s = 0.0f;
+    bool twice = false;
+    // the warp of this CTA that holds class v, kMaxWarps: none
+    auto holder = [&](int v) {
+        const int at = (v >> 3) - rank * p.vp;
+        return v >= 0 && at >= 0 && at < p.vp ? at / p.wv : kMaxWarps;
+    };
     for (int j = lane; j < p.K; j += 32) {
-        const float w = ent[j].v >= 0 ? ex2_approx((ent[j].q - top) * p.k) : 0.0f;
-        ent[j].q = w;
+        const int v = ent.v[j];
+        const int hw = holder(v);
+        if (hw < kMaxWarps) ent.sum[j] = __int_as_float(atomicAdd(ent.first + hw, 1));      // its place in the warp's list
+        float w = 0.0f;
+        if (v >= 0) {
+            w = ex2_approx((ent.q[j] - top) * p.k);
+            for (unsigned h = (unsigned)v * 2654435761u;; h += 1u << 21) {      // the top 11 bits choose the slot
+                const int was = atomicCAS(table + ((h >> 21) & (unsigned)(slots - 1)), kNoClass, v);
+                if (was == kNoClass) break;
+                if (was == v) {
+                    twice = true;
+                    break;
+                }
+            }
+        }
+        ent.q[j] = w;
         s += w;
     }
     s = wsum(s);
-    const float inv = __fdiv_rn(1.0f, s);
-    for (int j = lane; j < p.K; j += 32) ent[j].q = ent[j].v >= 0 ? ent[j].q * inv : 0.0f;
-    if (lane == 0) *live = any ? 1 : 0;
     __syncwarp();
+    const int n = lane < kMaxWarps ? ent.first[lane] : 0;
+    int before = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int up = __shfl_up_sync(0xFFFFFFFFu, before, o);
+        if (lane >= o) before += up;
+    }
+    __syncwarp();
+    if (lane <= kMaxWarps) ent.first[lane] = before - n;      // lane kMaxWarps: all of them
+    __syncwarp();
+    const float inv = __fdiv_rn(1.0f, s);
+    for (int j = lane; j < p.K; j += 32) {
+        const int hw = holder(ent.v[j]);
+        if (hw < kMaxWarps) ent.order[ent.first[hw] + __float_as_int(ent.sum[j])] = j;
+        const float q = ent.v[j] >= 0 ? ent.q[j] * inv : 0.0f;
+        ent.q[j] = q;
+        ent.sum[j] = q;
+    }
+    __syncwarp();
+    if (__any_sync(0xFFFFFFFFu, twice)) {
+        for (int j = lane; j < p.K; j += 32) {
+            const int v = ent.v[j];
+            float q = 0.0f;
+            for (int i = 0; i < p.K; i++)
+                if (ent.v[i] == v) q += ent.q[i];
+            ent.sum[j] = q;
+        }
+        __syncwarp();
+    }
+    return __any_sync(0xFFFFFFFFu, any);
 }
-__device__ __forceinline__ void write_loss(const DistillArgs &p, int row, const Entry *ent, bool live, float2 pr)
+__device__ __forceinline__ void write_loss(const DistillArgs &p, int row, const Entries &ent, bool live, float2 pr)
 {
     const int lane = threadIdx.x & 31;
     constexpr float LN2 = 0.69314718055994531f;
     const float l2s = log2f(pr.y);
+    const uint16_t *zr = p.z + (size_t)row * p.ldz;
     float l = 0.0f;
+#pragma unroll 4
     for (int j = lane; j < p.K; j += 32) {
-        const Entry e = ent[j];
+        const float q = ent.q[j];
+        const int v = ent.v[j];
         // log2 q - log2 p; a probability of zero (or none) adds nothing
-        if (e.v >= 0 && !(e.q == 0.0f)) l += e.q * ((log2f(e.q) + l2s) - fmaf(e.z, p.k, -pr.x));
+        if (v >= 0 && !(q == 0.0f)) {
+            // a CTA that holds the whole row has kept the logits; in a cluster they are read again
+            const float z = p.cl == 1 ? ent.z[j] : h2f(zr[v]);
+            l += q * ((log2f(q) + l2s) - fmaf(z, p.k, -pr.x));
+        }
     }
     l = wsum(l);
     if (lane == 0) p.row_loss[row] = live ? l * LN2 * p.tau * p.tau : 0.0f;
 }
 
-__device__ __forceinline__ void bulk_in(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
+// Bulk copies with an L2 eviction priority (l2_policy)
+__device__ __forceinline__ void bulk_in(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar, uint64_t policy)
 {
     mbar_arrive_expect_tx(bar, bytes);
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-                 "r"(bytes), "r"(bar)
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst),
+                 "l"(src), "r"(bytes), "r"(bar), "l"(policy)
                  : "memory");
 }
-__device__ __forceinline__ void bulk_out(void *dst, uint32_t src, uint32_t bytes)
+__device__ __forceinline__ void bulk_out(void *dst, uint32_t src, uint32_t bytes, uint64_t policy)
 {
-    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group.L2::cache_hint [%0], [%1], %2, %3;" ::"l"(dst), "r"(src), "r"(bytes),
+                 "l"(policy)
+                 : "memory");
 }
 
-// Shared memory: buffers [nw][ns][per] of 16-byte vectors | mbarriers [nw][ns] | pairs [2][cl * nw] |
-// entries [3][K] | live [3] | abort word
+// Shared memory: buffers [nw][ns][per] of 16-byte vectors | entries [nb] | mbarriers: [nw][ns] of the buffers, [4] of
+// the pairs, 2 x [nb] of the entries (full, empty) | pairs [4][cl * nw] | hash tables [teachers] | the row's pair [nb] |
+// live [nb] | abort word
 struct Layout {
-    uint32_t bars, red, ent, live, abort, total;
+    uint32_t ent, bars, red, table, pair, live, abort, total;
+    int slots;
 };
-__host__ __device__ inline Layout layout_of(int nw, int ns, int per, int cl, int K)
+__host__ __device__ inline Layout layout_of(int nw, int ns, int per, int cl, int K, int nb)
 {
     Layout l;
     uint32_t at = (uint32_t)nw * (uint32_t)ns * (uint32_t)per * 16u;
-    l.bars = at;
-    at += (uint32_t)nw * (uint32_t)ns * 8u;
-    l.red = at;
-    at += 2u * (uint32_t)cl * (uint32_t)nw * 8u;
     l.ent = at;
-    at += (uint32_t)kEntryBuffers * (uint32_t)K * (uint32_t)sizeof(Entry);
+    at += (uint32_t)nb * ((uint32_t)K * kEntryWords + kMaxWarps + 1u) * 4u;
+    at = (at + 7u) & ~7u;
+    l.bars = at;
+    at += ((uint32_t)nw * (uint32_t)ns + (uint32_t)kPairBuffers + 2u * (uint32_t)nb) * 8u;
+    l.red = at;
+    at += (uint32_t)kPairBuffers * (uint32_t)cl * (uint32_t)nw * 8u;
+    l.slots = 32;
+    while (l.slots < 2 * K) l.slots *= 2;
+    l.table = at;
+    at += (uint32_t)kTeachers * 4u * (uint32_t)l.slots;
+    l.pair = at;
+    at += 8u * (uint32_t)nb;
     l.live = at;
-    at += 4u * kEntryBuffers;
+    at += 4u * (uint32_t)nb;
     l.abort = at;
     at += 4u;
     l.total = (at + 15u) & ~15u;
     return l;
 }
 
-// BULK: rows start on 16-byte boundaries and move by bulk copies (a last, partial vector by element accesses);
-// otherwise the warp copies elements.  STREAM: the row does not stay in shared memory; the second pass reads it again.
-template <bool BULK, bool STREAM>
-__global__ void __launch_bounds__(1024, 1) k_distill(const DistillArgs p)
+// Bounded wait that sleeps between its tries: a warp that polls takes the issue slots of those that work (and of the
+// teacher's warps above all, which everybody then waits for longer).
+template <bool CLUSTER>
+static __device__ __noinline__ bool wait_asleep(uint32_t bar, uint32_t parity, volatile uint32_t *abort_flag)
 {
-    pdl_trigger();
-    pdl_wait();
-    extern __shared__ __align__(128) uint8_t smem[];
-    const int per = STREAM ? p.chunk : p.wv;
-    const Layout L = layout_of(p.nw, p.ns, per, p.cl, p.K);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int rank = p.cl > 1 ? (int)cluster_ctarank() : 0;
-    const int cluster = blockIdx.x / p.cl, clusters = gridDim.x / p.cl;
-    const int n_rows = cluster < p.B ? (p.B - 1 - cluster) / clusters + 1 : 0;
-    float2 *red = (float2 *)(smem + L.red);
-    Entry *entries = (Entry *)(smem + L.ent);
-    int *live = (int *)(smem + L.live);
-    volatile uint32_t *abort_flag = (volatile uint32_t *)(smem + L.abort);
-    const int pairs = p.cl * p.nw;
-
-    if (warp < p.nw && lane == 0)
-        for (int s = 0; s < p.ns; s++) mbar_init(smem_u32(smem + L.bars) + 8u * (uint32_t)(warp * p.ns + s), 1);
-    if (threadIdx.x == 0) *abort_flag = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    __syncthreads();
-    cluster_sync_all();              // every CTA of the cluster runs before anything is written into its shared memory
-    if (n_rows == 0) return;         // the same for all CTAs of a cluster
-
-    if (warp == p.nw) {
-        // ------------------------------------------------------------ the teacher's entries, the losses
-        prepare_entries(p, cluster, entries, live);
-        cluster_arrive();
-        for (int i = 0; i < n_rows; i++) {
-            cluster_wait();
-            if (rank == 0) {
-                const int b = i % kEntryBuffers;
-                write_loss(p, cluster + i * clusters, entries + b * p.K, live[b] != 0, row_pair(red + (i & 1) * pairs, pairs));
-            }
-            if (i + 1 < n_rows) {
-                // after the barrier of row i all warps have finished with row i - 2, whose buffer this is
-                const int b = (i + 1) % kEntryBuffers;
-                prepare_entries(p, cluster + (i + 1) * clusters, entries + b * p.K, live + b);
-                cluster_arrive();
-            }
+    unsigned long long t0 = 0;
+    for (uint32_t it = 0;; ++it) {
+        __nanosleep(kNap);
+        if (CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity)) return true;
+        if ((it & 63u) == 63u) {
+            if (*abort_flag) return false;
+            const unsigned long long now = global_ns();
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > WAIT_LIMIT_NS) return false;
         }
-        return;
     }
+}
 
-    // ---------------------------------------------------------------- this warp's part of every row
-    const int cv = (p.C + 7) / 8;
-    int v0 = rank * p.vp + warp * p.wv;
-    const int v_end = min(cv, (rank + 1) * p.vp);
-    const int nv = max(0, min(v_end, v0 + p.wv) - v0);
-    if (nv == 0) v0 = 0;
-    uint4 *buf = (uint4 *)smem + (size_t)warp * p.ns * per;
-    const uint32_t bar0 = smem_u32(smem + L.bars) + 8u * (uint32_t)(warp * p.ns);
+// What all warps of a CTA share, and each warp's part of the rows.  BULK: rows start on 16-byte boundaries and move by
+// bulk copies (a last, partial vector by element accesses); otherwise the warp copies elements.
+template <bool BULK>
+struct Cta {
+    const DistillArgs &p;
+    uint8_t *smem;
+    Layout L;
+    int warp, lane, rank, cluster, clusters, n_rows, pairs;
+    uint32_t bars;
+    volatile uint32_t *abort_flag;
     bool dead = false;
+    // this warp's part: vectors [v0, v0 + nv) of a row, its buffers and their mbarriers
+    int v0, nv;
+    uint4 *buf;
+    uint32_t bar0;
 
-    // requests vectors [f, f + n) of this warp's part of row i into buffer s (the caller knows that it is free)
-    auto request = [&](int i, int s, int f, int n) {
-        const int row = cluster + i * clusters;
-        const uint16_t *src = p.z + (size_t)row * p.ldz + (size_t)(v0 + f) * 8;
-        uint4 *dst = buf + s * per;
-        const int whole = min(n, p.C / 8 - (v0 + f));             // n - 1 where the part ends in a partial vector
+    __device__ __forceinline__ Cta(const DistillArgs &args, uint8_t *s) : p(args), smem(s), L(layout_of(args.nw, args.ns, args.per, args.cl, args.K, 1 << args.nb_log2))
+    {
+        warp = threadIdx.x >> 5;
+        lane = threadIdx.x & 31;
+        rank = p.cl > 1 ? (int)cluster_ctarank() : 0;
+        cluster = (int)blockIdx.x / p.cl;
+        clusters = (int)gridDim.x / p.cl;
+        n_rows = cluster < p.B ? (p.B - 1 - cluster) / clusters + 1 : 0;
+        pairs = p.cl * p.nw;
+        bars = smem_u32(smem + L.bars);
+        abort_flag = (volatile uint32_t *)(smem + L.abort);
+        const int v_end = min((p.C + 7) / 8, (rank + 1) * p.vp);
+        v0 = rank * p.vp + warp * p.wv;
+        nv = warp < p.nw ? max(0, min(v_end, v0 + p.wv) - v0) : 0;
+        if (nv == 0) v0 = 0;
+        buf = (uint4 *)smem + (size_t)warp * p.ns * p.per;
+        bar0 = bars + 8u * (uint32_t)(warp * p.ns);
+        if (warp < p.nw && lane == 0)
+            for (int i = 0; i < p.ns; i++) mbar_init(bar0 + 8u * (uint32_t)i, 1);
+        if (threadIdx.x == 0) {
+            for (int i = 0; i < kPairBuffers; i++) mbar_init(pair_bar(i), (uint32_t)pairs);
+            for (int b = 0; b < 1 << p.nb_log2; b++) {
+                mbar_init(full_bar(b), 1);
+                mbar_init(empty_bar(b), (uint32_t)p.nw);
+            }
+            *abort_flag = 0;
+        }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
+        if (p.cl > 1) cluster_sync_all();   // every CTA of the cluster has its barriers before anything arrives there
+    }
+    __device__ __forceinline__ uint32_t pair_bar(int i) const { return bars + 8u * (uint32_t)(p.nw * p.ns + (i & (kPairBuffers - 1))); }
+    __device__ __forceinline__ uint32_t full_bar(int b) const { return bars + 8u * (uint32_t)(p.nw * p.ns + kPairBuffers + b); }
+    __device__ __forceinline__ uint32_t empty_bar(int b) const { return full_bar(b) + (8u << p.nb_log2); }
+    __device__ __forceinline__ Entries entries(int b) const
+    {
+        float *at = (float *)(smem + L.ent) + b * (kEntryWords * p.K + kMaxWarps + 1);
+        return {(int32_t *)at, at + p.K, at + 2 * p.K, at + 3 * p.K, (int32_t *)(at + 4 * p.K), (int32_t *)(at + 5 * p.K)};
+    }
+    __device__ __forceinline__ float2 *pair_of(int b) const { return (float2 *)(smem + L.pair) + b; }
+    __device__ __forceinline__ int *live(int b) const { return (int *)(smem + L.live) + b; }
+    __device__ __forceinline__ float2 *red(int i) const { return (float2 *)(smem + L.red) + (i & (kPairBuffers - 1)) * pairs; }
+    __device__ __forceinline__ int row_of(int i) const { return cluster + i * clusters; }
+
+    // A wait of the whole warp; one that runs out ends all later ones of this CTA at once.
+    template <bool CLUSTER>
+    __device__ __forceinline__ void wait(uint32_t bar, uint32_t parity)
+    {
+        bool got = CLUSTER ? mbar_try_wait_cluster(bar, parity) : mbar_try_wait(bar, parity);
+        if (!got) got = wait_asleep<CLUSTER>(bar, parity, abort_flag);
+        if (!__all_sync(0xFFFFFFFFu, got)) {
+            if (lane == 0 && p.kerr && !*abort_flag) atomicCAS(p.kerr, 0u, (uint32_t)KERR_WAIT_FULL | 0x40u | ((uint32_t)blockIdx.x << 8));
+            *abort_flag = 1u;
+            dead = true;
+        }
+    }
+    // Requests vectors [f, f + n) of this warp's part of row i into buffer s (the caller knows that it is free).
+    __device__ __forceinline__ void request(int i, int s, int f, int n, uint64_t policy)
+    {
+        const uint16_t *src = p.z + (size_t)row_of(i) * p.ldz + (size_t)(v0 + f) * 8;
+        uint4 *dst = buf + s * p.per;
         if (BULK) {
-            if (lane == 0) {                                      // each use of a buffer completes one phase of its barrier
-                if (whole > 0) bulk_in(smem_u32(dst), src, (uint32_t)whole * 16u, bar0 + 8u * (uint32_t)s);
+            const int whole = min(n, p.C / 8 - (v0 + f));             // n - 1 where the part ends in a partial vector
+            if (lane == 0) {                                          // each use of a buffer completes one phase of its barrier
+                if (whole > 0) bulk_in(smem_u32(dst), src, (uint32_t)whole * 16u, bar0 + 8u * (uint32_t)s, policy);
                 else mbar_arrive(bar0 + 8u * (uint32_t)s);
             }
             if (whole < n && lane < 8) {
@@ -321,194 +487,322 @@ __global__ void __launch_bounds__(1024, 1) k_distill(const DistillArgs p)
                 ((uint16_t *)dst)[e] = (v0 + f) * 8 + e < p.C ? src[e] : (uint16_t)kNegInf16;
         }
         __syncwarp();
-    };
-    // waits for a buffer's n-th use to be filled
-    auto arrived = [&](int s, int use) {
+    }
+    __device__ __forceinline__ void arrived(int s, uint32_t parity)
+    {
+        if (BULK) wait<false>(bar0 + 8u * (uint32_t)s, parity);
+    }
+    // Writes this warp's gradient of row i from buffer s; commits one bulk group.
+    __device__ __forceinline__ void send(int i, int s, uint64_t policy)
+    {
+        uint16_t *dst = out(i);
+        const uint4 *src = buf + s * p.per;
         if (BULK) {
-            const bool got = mbar_wait(bar0 + 8u * (uint32_t)s, (uint32_t)(use & 1), (volatile uint32_t *)abort_flag);
-            if (!__all_sync(0xFFFFFFFFu, got)) {
-                if (lane == 0 && p.kerr && !*abort_flag) atomicCAS(p.kerr, 0u, (uint32_t)KERR_WAIT_FULL | 0x40u | ((uint32_t)blockIdx.x << 8));
-                *abort_flag = 1u;
-                dead = true;
-            }
-        }
-    };
-    // writes vectors [f, f + n) of the gradient of row i from buffer s; always commits a bulk group
-    auto send = [&](int i, int s, int f, int n) {
-        const int row = cluster + i * clusters;
-        uint16_t *dst = p.dz + (size_t)row * p.lddz + (size_t)(v0 + f) * 8;
-        const uint4 *src = buf + s * per;
-        const int whole = min(n, p.C / 8 - (v0 + f));
-        if (BULK) {
+            const int whole = min(nv, p.C / 8 - v0);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
-                if (whole > 0 && !dead) bulk_out(dst, smem_u32(src), (uint32_t)whole * 16u);
+                if (whole > 0 && !dead) bulk_out(dst, smem_u32(src), (uint32_t)whole * 16u, policy);
                 bulk_commit_group();
             }
-            if (whole < n && lane < 8 && !dead) {
-                const int e = (v0 + f + whole) * 8 + lane;
+            if (whole < nv && lane < 8 && !dead) {
+                const int e = (v0 + whole) * 8 + lane;
                 if (e < p.C) dst[whole * 8 + lane] = ((const uint16_t *)(src + whole))[lane];
             }
-            __syncwarp();
         } else {
             __syncwarp();
             if (!dead)
-                for (int e = lane; e < n * 8; e += 32)
-                    if ((v0 + f) * 8 + e < p.C) dst[e] = ((const uint16_t *)src)[e];
-            __syncwarp();
+                for (int e = lane; e < nv * 8; e += 32)
+                    if (v0 * 8 + e < p.C) dst[e] = ((const uint16_t *)src)[e];
         }
-    };
-    auto publish = [&](int i, const float2 pr) {
-        float2 *slot = red + (i & 1) * pairs + rank * p.nw + warp;
+        __syncwarp();
+    }
+    // Where this warp's gradient of row i goes.
+    __device__ __forceinline__ uint16_t *out(int i) const { return p.dz + (size_t)row_of(i) * p.lddz + (size_t)v0 * 8; }
+    // Zeros for this warp's part of a row without a teacher.
+    __device__ __forceinline__ void send_zeros(int i)
+    {
+        for (int j = lane; j < nv; j += 32) store8<BULK>(out(i) + j * 8, make_uint4(0u, 0u, 0u, 0u), (v0 + j) * 8, p.C);
+    }
+    // This warp's pair of row i to every CTA of the cluster.
+    __device__ __forceinline__ void publish(int i, float2 pr)
+    {
+        float2 *slot = red(i) + rank * p.nw + warp;
         if (p.cl == 1) {
-            if (lane == 0) *slot = pr;
+            if (lane == 0) {
+                *slot = pr;
+                mbar_arrive(pair_bar(i));
+            }
         } else if (lane < p.cl) {
             const uint32_t to = mapa_u32(smem_u32(slot), (uint32_t)lane);
             asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(pr.x), "f"(pr.y) : "memory");
+            mbar_arrive_cluster(mapa_u32(pair_bar(i), (uint32_t)lane));
         }
         __syncwarp();
-    };
-
-    if (!STREAM) {
-        // buffer of row i: i % ns.  Three buffers: row i + 2 is on its way while row i + 1 is summed and row i is
-        // turned into its gradient.  Two: row i + 2 is requested when row i has left.
-        auto first_pass = [&](int i) {
-            const int s = i % p.ns;
-            if (nv > 0) arrived(s, i / p.ns);
-            Run r;
-#pragma unroll 4
-            for (int j = lane; j < nv; j += 32) run_add8(r, buf[s * per + j], p.k);
-            return run_warp(r);
-        };
-        if (nv > 0) {
-            request(0, 0, 0, nv);
-            if (n_rows > 1) request(1, 1, 0, nv);
+    }
+    // The row's pair, once all warps have published theirs.
+    __device__ __forceinline__ float2 collect(int i)
+    {
+        const uint32_t parity = (uint32_t)(i / kPairBuffers) & 1u;
+        if (p.cl == 1) wait<false>(pair_bar(i), parity);
+        else wait<true>(pair_bar(i), parity);
+        return row_pair(red(i), pairs);
+    }
+    // The teacher's entries of row i.
+    __device__ __forceinline__ int open_entries(int i)
+    {
+        const int b = i & ((1 << p.nb_log2) - 1);
+        wait<false>(full_bar(b), (uint32_t)(i >> p.nb_log2) & 1u);
+        return b;
+    }
+    // ... are not needed any more by this warp; with them goes what the row's loss needs of the row.
+    __device__ __forceinline__ void close_entries(int b, float2 pr)
+    {
+        if (warp == 0 && lane == 0) *pair_of(b) = pr;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(empty_bar(b));
+    }
+    // Row i's list on its way to L2: with all SMs' copies queued at the memory a load takes longer than a row.
+    __device__ __forceinline__ void prefetch_list(int i)
+    {
+        if (i >= n_rows) return;
+        const size_t at = (size_t)row_of(i) * p.ldt;
+        for (int j = lane * 32; j < p.K; j += 1024) {
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(p.idx + at + j));
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(p.t + at + j));
         }
-        publish(0, first_pass(0));
-        cluster_arrive();
-        for (int i = 0; i < n_rows; i++) {
-            if (p.ns > 2 && i + 2 < n_rows && nv > 0) {
-                if (lane == 0) bulk_wait_group_read<0>();          // row i - 1 has left this buffer (sent an iteration ago)
+    }
+    // The work of the last kTeachers warps: the entries of every kTeachers-th row, as far ahead as there are buffers, and
+    // the row's loss when a buffer comes back.
+    __device__ __forceinline__ void teach()
+    {
+        const int me = warp - p.nw, nb = 1 << p.nb_log2;
+        for (int i = me; i < n_rows + nb; i += kTeachers) {
+            const int b = i & (nb - 1);
+            const uint32_t parity = ((uint32_t)(i >> p.nb_log2) & 1u) ^ 1u;
+            // this wait is long and nothing hurries: sleep between the tries, the issue slots belong to the others
+            for (int tries = 0; tries < 1000000 && !mbar_try_wait(empty_bar(b), parity) && !*abort_flag; tries++) __nanosleep(200);
+            wait<false>(empty_bar(b), parity);
+            if (i >= nb && rank == 0 && !dead) write_loss(p, row_of(i - nb), entries(b), *live(b) != 0, *pair_of(b));
+            if (i < n_rows) {
                 __syncwarp();
-                request(i + 2, (i + 2) % p.ns, 0, nv);
-            }
-            float2 next = make_float2(0.0f, 0.0f);
-            if (i + 1 < n_rows) next = first_pass(i + 1);
-            cluster_wait();
-            const float2 pr = row_pair(red + (i & 1) * pairs, pairs);
-            const int eb = i % kEntryBuffers;
-            const bool alive = live[eb] != 0;
-            if (i + 1 < n_rows) {
-                publish(i + 1, next);
-                cluster_arrive();
-            }
-            if (p.dz && nv > 0) {
-                uint4 *v = buf + (i % p.ns) * per;
-                grad_vectors(v, nv, p.k, pr, p.c, alive);
-                __syncwarp();
-                if (alive) patch_targets((uint16_t *)v, v0 * 8, nv * 8, entries + eb * p.K, p.K, p.k, pr, p.c);
-                send(i, i % p.ns, 0, nv);
-            }
-            if (p.ns == 2 && i + 2 < n_rows && nv > 0) {
-                if (lane == 0) bulk_wait_group_read<0>();
-                __syncwarp();
-                request(i + 2, i % 2, 0, nv);
-            }
-        }
-    } else {
-        // Chunks of this warp's part go through a ring of ns buffers in the order in which they are used: the first
-        // pass over row 0, then for each row i the first pass over row i + 1 and the second over row i.  Requests run
-        // ns - 2 chunks ahead, so a buffer's previous gradient has had one chunk's time to leave.
-        const int nch = (nv + per - 1) / per;
-        const int passes = p.dz ? 2 : 1;
-        const int total = nch * n_rows * passes;
-        int asked = 0, used = 0;
-        auto ask = [&](int q) {           // chunk q of the sequence
-            const int pass = q / nch, ch = q - pass * nch;
-            int row;
-            if (passes == 1 || pass == 0) row = pass;
-            else if (pass == 2 * n_rows - 1) row = n_rows - 1;
-            else row = (pass & 1) ? (pass + 1) / 2 : pass / 2 - 1;
-            request(row, q % p.ns, ch * per, min(per, nv - ch * per));
-        };
-        auto ahead = [&]() {
-            for (; asked < total && asked < used + p.ns - 1; asked++) {
-                if (lane == 0) bulk_wait_group_read<1>();
-                __syncwarp();
-                ask(asked);
-            }
-        };
-        auto first_pass = [&]() {
-            Run r;
-            for (int ch = 0; ch < nch; ch++, used++) {
-                ahead();
-                const int n = min(per, nv - ch * per), s = used % p.ns;
-                arrived(s, used / p.ns);
-#pragma unroll 4
-                for (int j = lane; j < n; j += 32) run_add8(r, buf[s * per + j], p.k);
-                __syncwarp();
-                if (lane == 0) bulk_commit_group();       // an empty group: every chunk counts as one
-            }
-            return run_warp(r);
-        };
-        publish(0, first_pass());
-        cluster_arrive();
-        for (int i = 0; i < n_rows; i++) {
-            float2 next = make_float2(0.0f, 0.0f);
-            if (i + 1 < n_rows) next = first_pass();
-            cluster_wait();
-            const float2 pr = row_pair(red + (i & 1) * pairs, pairs);
-            const int eb = i % kEntryBuffers;
-            const bool alive = live[eb] != 0;
-            if (i + 1 < n_rows) {
-                publish(i + 1, next);
-                cluster_arrive();
-            }
-            if (p.dz) {
-                for (int ch = 0; ch < nch; ch++, used++) {
-                    ahead();
-                    const int n = min(per, nv - ch * per), s = used % p.ns;
-                    arrived(s, used / p.ns);
-                    uint4 *v = buf + s * per;
-                    grad_vectors(v, n, p.k, pr, p.c, alive);
-                    __syncwarp();
-                    if (alive) patch_targets((uint16_t *)v, (v0 + ch * per) * 8, n * 8, entries + eb * p.K, p.K, p.k, pr, p.c);
-                    send(i, s, ch * per, n);
+                if (i == me)
+                    for (int r = 1; r < kAhead; r++) prefetch_list(i + r * kTeachers);
+                prefetch_list(i + kAhead * kTeachers);
+                const bool any = prepare_entries(p, row_of(i), rank, entries(b), (int *)(smem + L.table) + me * L.slots, L.slots);
+                if (lane == 0) {
+                    *live(b) = any ? 1 : 0;
+                    mbar_arrive(full_bar(b));
                 }
             }
         }
     }
-    if (lane == 0) {
-        bulk_wait_group_read<0>();          // shared memory must outlive the copies that read it
-        if (dead) {                         // ... and, after a wait that ran out, those still on their way into it (bounded)
-            const unsigned long long t0 = global_ns();
-            while (global_ns() - t0 < 1000000ull) {}
+    // Common end: shared memory outlives the copies that read it, those still on their way into it after a wait that
+    // ran out (for a bounded time), and the other CTAs' stores.
+    __device__ __forceinline__ void leave()
+    {
+        if (lane == 0) {
+            bulk_wait_group_read<0>();
+            if (dead) {
+                const unsigned long long t0 = global_ns();
+                while (global_ns() - t0 < 1000000ull) {}
+            }
+        }
+        __syncwarp();
+        if (p.cl > 1) cluster_sync_all();
+    }
+};
+
+// Rows whose exponentials stay in registers: R vectors per lane.
+template <int R, bool BULK>
+__global__ void __launch_bounds__((kMaxWarps + kTeachers) * 32, 1) k_distill(const DistillArgs p)
+{
+    pdl_trigger();
+    pdl_wait();
+    extern __shared__ __align__(128) uint8_t smem[];
+    Cta<BULK> c(p, smem);
+    if (c.warp >= p.nw) {
+        c.teach();
+        c.leave();
+        return;
+    }
+    const uint64_t policy = l2_policy(2);        // every byte is used once
+    const int nv = c.nv;
+    int s_ask = 0, s_use = 0;
+    uint32_t parity = 0;
+    auto ask = [&](int i) {
+        if (nv > 0 && i < c.n_rows) {
+            c.request(i, s_ask, 0, nv, policy);
+            s_ask = s_ask + 1 == p.ns ? 0 : s_ask + 1;
+        }
+    };
+    for (int i = 0; i + 1 < p.ns; i++) ask(i);
+    for (int i = 0; i < c.n_rows; i++) {
+        // the buffer that row i + ns - 1 goes into held row i - 1, whose gradient has had most of this iteration to leave it
+        uint4 *v = c.buf + s_use * p.per;
+        float e[R][8];
+        float m = -INFINITY, b = 0.0f, s = 0.0f;
+        if (nv > 0) {
+            c.arrived(s_use, parity);
+            uint4 x[R];
+            __half2 mx = __half2half2(__ushort_as_half((unsigned short)kNegInf16));
+#pragma unroll
+            for (int u = 0; u < R; u++) {
+                const int j = c.lane + 32 * u;
+                x[u] = j < nv ? v[j] : make_uint4(0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u);
+                mx = __hmax2(mx, max8(x[u]));
+            }
+            m = fmaxf(__low2float(mx), __high2float(mx));           // NaN is dropped here and comes back in the sum
+            b = m == -INFINITY ? 0.0f : -__fmul_rn(m, p.k);
+            float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int u = 0; u < R; u++) {
+                const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+                for (int q = 0; q < 4; q++) {
+                    const float2 f = __half22float2(*(const __half2 *)&w[q]);
+                    e[u][2 * q] = ex2_approx(fmaf(f.x, p.k, b));
+                    e[u][2 * q + 1] = ex2_approx(fmaf(f.y, p.k, b));
+                    a[q] += e[u][2 * q] + e[u][2 * q + 1];
+                }
+            }
+            s = (a[0] + a[1]) + (a[2] + a[3]);
+        }
+        c.publish(i, warp_pair(m == -INFINITY ? -INFINITY : -b, s));
+        const int eb = c.open_entries(i);
+        const Entries ent = c.entries(eb);
+        if (nv > 0) keep_targets((const uint16_t *)v, c.v0 * 8, nv * 8, ent, c.warp);
+        __syncwarp();
+        const float2 pr = c.collect(i);
+        if (p.dz && nv > 0) {
+            const float cs = __fdiv_rn(p.c, pr.y);
+            if (*c.live(eb)) {
+                // this lane's exponentials are relative to 2^-b: a lane of nothing but -inf has zeros (or NaN)
+                const float k = m == -INFINITY ? cs * 0.0f : cs * ex2_approx(-b - pr.x);
+#pragma unroll
+                for (int u = 0; u < R; u++) {
+                    const int j = c.lane + 32 * u;
+                    if (j < nv)
+                        v[j] = make_uint4(pack_f16x2(e[u][0] * k, e[u][1] * k), pack_f16x2(e[u][2] * k, e[u][3] * k),
+                                          pack_f16x2(e[u][4] * k, e[u][5] * k), pack_f16x2(e[u][6] * k, e[u][7] * k));
+                }
+                __syncwarp();
+                patch_targets((uint16_t *)v, c.v0 * 8, nv * 8, ent, c.warp, p.k, pr, cs, p.c);
+            } else {
+                for (int j = c.lane; j < nv; j += 32) v[j] = make_uint4(0u, 0u, 0u, 0u);
+            }
+        }
+        if (nv > 0 && i + p.ns - 1 < c.n_rows) {
+            if (c.lane == 0) bulk_wait_group_read<0>();
+            __syncwarp();
+            ask(i + p.ns - 1);
+        }
+        if (p.dz && nv > 0) c.send(i, s_use, policy);
+        c.close_entries(eb, pr);
+        if (++s_use == p.ns) {
+            s_use = 0;
+            parity ^= 1u;
         }
     }
+    c.leave();
+}
+
+// Rows that are read twice.  Chunks of this warp's part go through a ring of ns buffers in the order in which they are
+// used, first pass and second pass of one row after the other, requested ns - 1 ahead.
+template <bool BULK>
+__global__ void __launch_bounds__((kMaxWarps + kTeachers) * 32, 1) k_distill_stream(const DistillArgs p)
+{
+    pdl_trigger();
+    pdl_wait();
+    extern __shared__ __align__(128) uint8_t smem[];
+    Cta<BULK> c(p, smem);
+    if (c.warp >= p.nw) {
+        c.teach();
+        c.leave();
+        return;
+    }
+    const uint64_t stay = l2_policy(1), go = l2_policy(2);
+    const int nv = c.nv, per = p.per, nch = (nv + per - 1) / per;
+    const bool twice = p.dz != nullptr;
+    int ask_row = 0, ask_ch = 0, ask_pass = 0, s_ask = 0, s_use = 0, ahead = 0;
+    uint32_t parity = 0;
+    auto ask = [&]() {
+        while (ahead < p.ns - 1 && nv > 0 && ask_row < c.n_rows) {
+            c.request(ask_row, s_ask, ask_ch * per, min(per, nv - ask_ch * per), ask_pass || !twice ? go : stay);
+            s_ask = s_ask + 1 == p.ns ? 0 : s_ask + 1;
+            ahead++;
+            if (++ask_ch == nch) {
+                ask_ch = 0;
+                if (twice && !ask_pass) ask_pass = 1;
+                else {
+                    ask_pass = 0;
+                    ask_row++;
+                }
+            }
+        }
+    };
+    auto consumed = [&]() {
+        ahead--;
+        if (++s_use == p.ns) {
+            s_use = 0;
+            parity ^= 1u;
+        }
+    };
+    for (int i = 0; i < c.n_rows; i++) {
+        Run r;
+        for (int ch = 0; ch < nch; ch++) {
+            ask();
+            c.arrived(s_use, parity);
+            run_vectors(r, c.buf + s_use * per, min(per, nv - ch * per), p.k);
+            __syncwarp();
+            consumed();
+        }
+        c.publish(i, warp_pair(r.m == -INFINITY ? -INFINITY : -r.b, r.s));
+        ask();
+        const float2 pr = c.collect(i);
+        const int eb = c.open_entries(i);
+        if (twice) {
+            const Entries ent = c.entries(eb);
+            const bool alive = *c.live(eb) != 0;
+            const float cs = __fdiv_rn(p.c, pr.y);
+            for (int ch = 0; ch < nch; ch++) {
+                ask();
+                c.arrived(s_use, parity);
+                const int n = min(per, nv - ch * per), first = (c.v0 + ch * per) * 8;
+                const uint4 *v = c.buf + s_use * per;
+                uint16_t *dst = c.out(i) + ch * per * 8;
+                if (alive && !c.dead) {
+                    grad_vectors<BULK>(v, n, dst, first, p.C, p.k, pr, cs);
+                    keep_targets((const uint16_t *)v, first, n * 8, ent, c.warp);
+                    __syncwarp();              // orders the warp's stores: the targets' come after those around them
+                    patch_targets(dst, first, n * 8, ent, c.warp, p.k, pr, cs, p.c);
+                }
+                __syncwarp();
+                consumed();
+            }
+            if (!alive && !c.dead) c.send_zeros(i);
+        }
+        c.close_entries(eb, pr);
+    }
+    c.leave();
 }
 
 constexpr uint32_t kSmemLimit = 220u * 1024u;
-constexpr int kMaxWarps = 31;
 
-template <bool BULK, bool STREAM>
-cudaError_t run(const DistillArgs &p, uint32_t smem, cudaStream_t st)
+typedef void (*DistillKernel)(const DistillArgs);
+
+// id: a number of its own for each kernel (what is known about it is kept per device)
+cudaError_t run(DistillKernel kern, int id, const DistillArgs &p, uint32_t smem, cudaStream_t st)
 {
-    static bool configured[kMaxDevices] = {};
+    static bool configured[kMaxDevices][32] = {};
+    static int resident[kMaxDevices][9] = {};       // clusters of a size that the device holds, one CTA per SM; 0 = not asked yet
     const int dev = current_device_slot();
     if (dev < 0) return cudaErrorInvalidDevice;
-    auto kern = k_distill<BULK, STREAM>;
-    if (!configured[dev]) {
+    if (!configured[dev][id]) {
         const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit);
         if (e != cudaSuccess) return e;
-        configured[dev] = true;
+        configured[dev][id] = true;
     }
-    const int threads = (p.nw + 1) * 32;
-    int per_sm = 2048 / threads;
-    const int by_smem = (int)((227u * 1024u) / (smem + 1024u));
-    if (by_smem < per_sm) per_sm = by_smem;
-    if (per_sm > 16) per_sm = 16;
-    if (per_sm < 1) per_sm = 1;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -519,12 +813,11 @@ cudaError_t run(const DistillArgs &p, uint32_t smem, cudaStream_t st)
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.stream = st;
     cfg.attrs = attr;
-    // Clusters the device holds with one CTA on each SM: rows are dealt out statically, so a cluster that had to
-    // wait for another to end would double the time.
-    static int resident[kMaxDevices][9] = {};       // 0 = not asked yet
+    // Rows are dealt out statically, so a cluster that had to wait for another to end would double the time: no more
+    // clusters than are resident at once.
     if (resident[dev][p.cl] == 0) {
         cfg.gridDim = dim3((unsigned)(148 / p.cl * p.cl));
-        cfg.blockDim = dim3(1024);
+        cfg.blockDim = dim3((kMaxWarps + kTeachers) * 32);
         cfg.dynamicSmemBytes = kSmemLimit;
         cfg.numAttrs = 1;
         int n = 0;
@@ -533,6 +826,11 @@ cudaError_t run(const DistillArgs &p, uint32_t smem, cudaStream_t st)
         if (n < 1) return cudaErrorLaunchOutOfResources;
         resident[dev][p.cl] = n;
     }
+    const int threads = (p.nw + kTeachers) * 32;
+    int per_sm = (kMaxWarps + kTeachers) * 32 / threads;          // what the kernel's registers allow
+    const int by_smem = (int)((227u * 1024u) / (smem + 1024u));
+    if (by_smem < per_sm) per_sm = by_smem;
+    if (per_sm < 1) per_sm = 1;
     int clusters = resident[dev][p.cl] * per_sm;
     if (clusters > p.B) clusters = p.B;
     cfg.gridDim = dim3((unsigned)(clusters * p.cl));
@@ -542,39 +840,46 @@ cudaError_t run(const DistillArgs &p, uint32_t smem, cudaStream_t st)
     return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
-// Vectors of a CTA over its warps: as few rounds of 32 lanes as 31 warps allow, then no more warps than that needs.
-void split_warps(DistillArgs &p, int vectors_per_cta, int unit)
+template <bool BULK>
+cudaError_t launch_rounds(int rounds, const DistillArgs &p, uint32_t smem, cudaStream_t st)
 {
-    p.vp = vectors_per_cta;
-    const int rounds = (p.vp + kMaxWarps * unit - 1) / (kMaxWarps * unit);
-    p.wv = (rounds < 1 ? 1 : rounds) * unit;
-    p.nw = (p.vp + p.wv - 1) / p.wv;
+    static const DistillKernel kern[kMaxRounds] = {k_distill<1, BULK>, k_distill<2, BULK>, k_distill<3, BULK>, k_distill<4, BULK>,
+                                                   k_distill<5, BULK>, k_distill<6, BULK>, k_distill<7, BULK>, k_distill<8, BULK>};
+    return run(kern[rounds - 1], (BULK ? 0 : kMaxRounds) + rounds - 1, p, smem, st);
 }
 
 cudaError_t launch_distill(DistillArgs p, cudaStream_t st)
 {
     const bool bulk = (((uintptr_t)p.z | (uintptr_t)p.dz) & 15) == 0 && (p.ldz & 7) == 0 && (!p.dz || (p.lddz & 7) == 0);
     const int cv = (p.C + 7) / 8;
-    p.chunk = 0;
+    p.nb_log2 = p.K <= 256 ? 2 : 1;
     for (p.cl = 1; p.cl <= 8; p.cl *= 2) {
-        split_warps(p, (cv + p.cl - 1) / p.cl, 32);
+        p.vp = (cv + p.cl - 1) / p.cl;
         // few long rows: more SMs per row
         if (p.cl < 8 && (long)p.B * p.cl * 2 <= 148 && p.vp >= 512) continue;
+        // four vectors a lane where that leaves a row one warp at least, more only where kMaxWarps warps need it
+        int rounds = (p.vp + 32 * kMaxWarps - 1) / (32 * kMaxWarps);
+        if (rounds > kMaxRounds) continue;
+        if (rounds < 4) rounds = p.vp >= 128 ? 4 : (p.vp + 31) / 32;
+        p.wv = p.per = rounds * 32;
+        p.nw = (p.vp + p.wv - 1) / p.wv;
         for (p.ns = 3; p.ns >= 2; p.ns--) {
-            const uint32_t smem = layout_of(p.nw, p.ns, p.wv, p.cl, p.K).total;
-            if (smem <= kSmemLimit) return bulk ? run<true, false>(p, smem, st) : run<false, false>(p, smem, st);
+            const uint32_t smem = layout_of(p.nw, p.ns, p.per, p.cl, p.K, 1 << p.nb_log2).total;
+            if (smem <= kSmemLimit) return bulk ? launch_rounds<true>(rounds, p, smem, st) : launch_rounds<false>(rounds, p, smem, st);
         }
     }
-    p.cl = 8;
-    p.chunk = 128;
-    p.ns = 4;
-    split_warps(p, (cv + 7) / 8, p.chunk);
-    uint32_t smem = layout_of(p.nw, p.ns, p.chunk, p.cl, p.K).total;
-    if (smem > kSmemLimit) {
-        p.ns = 3;
-        smem = layout_of(p.nw, p.ns, p.chunk, p.cl, p.K).total;
+    p.cl = 4;
+    p.vp = (cv + p.cl - 1) / p.cl;
+    p.wv = (p.vp + kMaxWarps - 1) / kMaxWarps;
+    p.nw = (p.vp + p.wv - 1) / p.wv;
+    uint32_t smem = 0;
+    p.ns = 3;
+    for (p.per = kChunk; p.per >= 64; p.per -= 64) {      // long teacher lists leave less room
+        smem = layout_of(p.nw, p.ns, p.per, p.cl, p.K, 1 << p.nb_log2).total;
+        if (smem <= kSmemLimit) break;
     }
-    return bulk ? run<true, true>(p, smem, st) : run<false, true>(p, smem, st);
+    if (p.per < 64) return cudaErrorInvalidConfiguration;
+    return bulk ? run(k_distill_stream<true>, 2 * kMaxRounds, p, smem, st) : run(k_distill_stream<false>, 2 * kMaxRounds + 1, p, smem, st);
 }
 
 }  // namespace
