@@ -69,6 +69,7 @@ struct Params {
     // a unit leaves its raw FP32 accumulator in partial[part][M][ldp] and a second kernel adds the
     // parts in ascending order and applies the epilogue.  split_k == 1: off.
     int split_k;
+    int split_major;                 // units of one part are neighbours (they share its operands), not the parts of one tile
     float *partial;
     int ldp;
     // tail split: the tiles left over for a last, partly filled round are cut into tail_split units
@@ -117,8 +118,9 @@ __device__ __forceinline__ Unit unit_of(const Params &p, int u, int nkb)
     w.kb1 = nkb;
     w.tail_slot = -1;
     if (p.split_k > 1) {            // parts of one tile are neighbouring units: they run side by side
-        tile = u / p.split_k;
-        w.part = u - tile * p.split_k;
+        const int tiles = p.tiles_m * p.tiles_n;
+        tile = p.split_major ? u % tiles : u / p.split_k;
+        w.part = p.split_major ? u / tiles : u - tile * p.split_k;
         w.kb0 = (int)(((long long)nkb * w.part) / p.split_k);
         w.kb1 = (int)(((long long)nkb * (w.part + 1)) / p.split_k);
     } else if (u >= p.full_units && p.tail_split > 1) {
@@ -689,13 +691,15 @@ cudaError_t launch_gemm_tc2(int op, int M, int N, int K, const uint16_t *A, int 
     }
     p.full_units = p.num_units = 0;
     p.split_k = 1;
+    p.split_major = x.split > 0 ? 1 : 0;
     p.partial = nullptr;
     p.ldp = (N + 31) / 32 * 32;
     p.tail_split = 1;
     p.tail_partial = nullptr;
     if (!lstm && splitk_ws && (((uintptr_t)splitk_ws) & 15) == 0) {
         int split = 1;
-        tc2_split_plan(M, N, K, splitk_ws_bytes, &split, nullptr, nullptr);
+        if (x.split > 0) split = x.split;      // the caller has sized the scratch for it
+        else tc2_split_plan(M, N, K, splitk_ws_bytes, &split, nullptr, nullptr);
         if (split > 1) {
             p.split_k = split;
             p.partial = (float *)splitk_ws;

@@ -43,7 +43,8 @@ __device__ __forceinline__ float ex2(float x)
 __global__ void __launch_bounds__(256) k_ce_combine(const float2 *__restrict__ stats, int R, int V, int groups,
                                                     const int32_t *__restrict__ labels, const float *__restrict__ zlabel,
                                                     float2 *__restrict__ rowsum, float *__restrict__ row_loss, uint32_t *bad_labels,
-                                                    const uint16_t *__restrict__ x, int ldx, int H, uint16_t *__restrict__ xs)
+                                                    const uint16_t *__restrict__ x, int ldx, int H, uint16_t *__restrict__ xs,
+                                                    float *__restrict__ factor)
 {
     pdl_trigger();
     pdl_wait();
@@ -92,51 +93,59 @@ __global__ void __launch_bounds__(256) k_ce_combine(const float2 *__restrict__ s
         if (good) row_loss[row] = (float)(((double)m - (double)zlabel[row] * (double)kLog2e + log2((double)s)) * 0.69314718055994530942);
         else row_loss[row] = 0.0f;                      // contributes neither loss nor gradient
         if (!good && bad_labels) atomicAdd(bad_labels, 1u);
+        red[0][r] = make_float2(m, good ? s : INFINITY);     // an ignored row's factors are zeros
+    }
+    if (!factor) return;
+    // what turns a group's exponentials into 2^14 p, a row's groups next to each other (the statistics come from L2 now)
+    __syncthreads();
+    m = red[0][r].x;
+    s = red[0][r].y;
+    if (row < R) {
+        const float inv = __fdiv_rn(1.0f, s);
+        float *f = factor + (size_t)row * groups;
+        for (int g = threadIdx.x >> 2; g < groups; g += 64) f[g] = s == INFINITY ? 0.0f : ex2((-stats[(size_t)g * R + row].y - m) + 14.0f) * inv;
     }
 }
 
-// e -> 2^14 (p - [v = y]) in place.  A warp takes 2048 columns of one row, 16 bytes a lane, all loads ahead of the
-// first use; the eight warps of a CTA take neighbouring rows, which share the sectors of `stats`.
-__global__ void __launch_bounds__(256) k_ce_rescale(uint16_t *__restrict__ e16, int ld, const float2 *__restrict__ stats, int R,
+// e -> 2^14 (p - [v = y]) in place.  A CTA takes 16384 neighbouring columns of one row (32 KB), 16 bytes a lane and
+// load, all loads ahead of the first use.
+__global__ void __launch_bounds__(256) k_ce_rescale(uint16_t *__restrict__ e16, int ld, const float *__restrict__ factor, int groups,
                                                     int V, const int32_t *__restrict__ labels, const float *__restrict__ zlabel,
                                                     const float2 *__restrict__ rowsum)
 {
     pdl_trigger();
     pdl_wait();
-    const int lane = threadIdx.x & 31, row = blockIdx.y * 8 + (threadIdx.x >> 5);
-    if (row >= R) return;
-    const int col0 = blockIdx.x * 2048 + lane * 8;
+    const int row = blockIdx.y, col0 = blockIdx.x * 16384 + threadIdx.x * 8;
     uint16_t *er = e16 + (size_t)row * ld;
-    const int y = labels[row];
-    const bool good = y >= 0 && y < V;
+    const float *fr = factor + (size_t)row * groups;
     uint4 v[8];
     float f[8];
-    const float2 sum = rowsum[row];
-    const float inv = __fdiv_rn(1.0f, sum.y);
 #pragma unroll
     for (int u = 0; u < 8; u++) {
-        const int col = col0 + u * 256;
-        if (good && col < ld) {
-            v[u] = *(const uint4 *)(er + col);
-            f[u] = stats[(size_t)(col / kGroup) * R + row].y;
+        const int col = col0 + u * 2048;
+        if (col < ld) {
+            v[u] = __ldcs((const uint4 *)(er + col));
+            f[u] = __ldg(fr + col / kGroup);
         }
     }
+    const int y = labels[row];           // asked for last: nothing waits for it before the row's loads are out
+    const bool good = y >= 0 && y < V;
 #pragma unroll
     for (int u = 0; u < 8; u++) {
-        const int col = col0 + u * 256;
+        const int col = col0 + u * 2048;
         if (col >= ld) continue;
         uint32_t w[4] = {0u, 0u, 0u, 0u};
         if (good) {
             const uint32_t x[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-            const float k = ex2((-f[u] - sum.x) + 14.0f) * inv;
 #pragma unroll
             for (int q = 0; q < 4; q++) {
                 const float2 t = __half22float2(*(const __half2 *)&x[q]);
-                const __half2 h = __floats2half2_rn(t.x * k, t.y * k);
+                const __half2 h = __floats2half2_rn(t.x * f[u], t.y * f[u]);
                 w[q] = *(const uint32_t *)&h;
             }
             if (y - col >= 0 && y - col < 8) {           // the label's element from its FP32 logit
-                const float p = ex2(fmaf(zlabel[row], kLog2e, -sum.x)) * inv;
+                const float2 sum = rowsum[row];
+                const float p = ex2(fmaf(zlabel[row], kLog2e, -sum.x)) * __fdiv_rn(1.0f, sum.y);
                 const uint32_t h = (uint32_t)__half_as_ushort(__float2half_rn((p - 1.0f) * 16384.0f));
 #pragma unroll
                 for (int q = 0; q < 4; q++) {
@@ -154,21 +163,38 @@ struct Plan {
     int lde;              // pitch of the exponentials
     int groups;
     int ldacc;
-    size_t e16, stats, rowsum, zlabel, xs, splitk, splitk_bytes, acc32, total;
+    size_t e16, stats, factor, rowsum, zlabel, xs, splitk, splitk_bytes, acc32, total;
 };
 
 // The split of dx's contraction over the vocabulary: for few rows the product has few tiles and reading W is what
 // takes time, so as many SMs as possible have to take part.
 constexpr int kDxSplit = 64;
 
+// dx of a few hundred to a few thousand rows: 256x256 tiles that do not fill the 74 CTA pairs, and a contraction of tens
+// of thousands.  As many parts of it as fit into one round of units, part by part, so that the tiles of a part walk
+// through the same operand panels side by side: 1024 x 1024 with K = 793471 (16 tiles) in 4 parts reads its operands
+// once from DRAM; in 9 parts, two rounds and 97 % of the pairs busy, the second round's units start apart and nothing is
+// shared any more (7.8 instead of 3.4 GB read, 1.53 ms); two pairs per tile in one cluster leave 57 % of the SMs idle
+// (1.82 ms).  A part keeps at least 64 k-blocks, under which the FP32 parts' way through L2 disappears.
+int dx_pair_split(int M, int N, int K)
+{
+    if (M < 256 || N < 256) return 0;
+    const int tiles = ((M + 255) / 256) * ((N + 255) / 256), nkb = (K + 63) / 64;
+    int s = tiles <= 37 ? 74 / tiles : 0;
+    if (s > 16) s = 16;
+    while (s > 1 && nkb / s < 64) s--;
+    return s > 1 ? s : 0;
+}
+
 size_t product_scratch(int op, int M, int N, int K, int max_split)
 {
+    if (op == MPT_OP_DGRAD)
+        if (const int s = dx_pair_split(M, N, K)) return (size_t)s * M * ((N + 31) / 32 * 32) * sizeof(float);
     if (tc4_split_for(M, N, K)) return 0;
     size_t need = 0;
     if (tc2_gemm_preferred(M, N, K)) return tc2_tail_ws_bytes(M, N, K);
     int bn, split;
     tc_gemm_plan(M, N, K, (size_t)1 << 40, &bn, &split, &need, nullptr, max_split);
-    (void)op;
     return need;
 }
 
@@ -186,6 +212,7 @@ Plan make_plan(int N, int V, int H, bool want_dx, bool want_dW, int row_block)
     const bool grads = want_dx || want_dW;
     p.e16 = take(grads ? (size_t)p.R * p.lde * 2 : 0);
     p.stats = take((size_t)p.groups * p.R * sizeof(float2));
+    p.factor = take(grads ? (size_t)p.groups * p.R * sizeof(float) : 0);
     p.rowsum = take((size_t)p.R * sizeof(float2));
     p.zlabel = take((size_t)p.R * sizeof(float));
     p.xs = take(want_dW ? (size_t)p.R * H * 2 : 0);
@@ -219,6 +246,13 @@ cudaError_t product(int op, int M, int N, int K, const uint16_t *A, int lda, con
         if (M > 128 && N >= 256 && tiles > 74)
             return launch_gemm_tc2(op, M, N, K, A, lda, B, ldb, C, ldc, false, nullptr, 0, nonfinite, status, st, nullptr, nullptr, 0, &x);
         return launch_gemm_tc(op, M, N, K, A, lda, B, ldb, C, ldc, false, nullptr, 0, nonfinite, status, st, nullptr, 0, nullptr, &x);
+    }
+    if (op == MPT_OP_DGRAD) {
+        if (const int s = dx_pair_split(M, N, K)) {
+            ProductExtra y = x;
+            y.split = s;
+            return launch_gemm_tc2(op, M, N, K, A, lda, B, ldb, C, ldc, false, nullptr, 0, nonfinite, status, st, nullptr, ws, ws_bytes, &y);
+        }
     }
     if (!x.acc32) {
         if (const int split = tc4_split_for(M, N, K))
@@ -265,6 +299,7 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
     float *zlabel = (float *)(ws + p.zlabel);
     uint16_t *xs = dW_dev ? (uint16_t *)(ws + p.xs) : nullptr;
     const bool grads = dx_dev || dW_dev;
+    float *factor = grads ? (float *)(ws + p.factor) : nullptr;
     cudaError_t e = cudaSuccess;
     if (bad_labels_dev) e = cudaMemsetAsync(bad_labels_dev, 0, sizeof(uint32_t), st);
     if (e == cudaSuccess && N == 0 && dW_dev) e = cudaMemset2DAsync(dW_dev, (size_t)lddw * 2, 0, (size_t)H * 2, (size_t)V, st);
@@ -279,10 +314,10 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
         e = product(MPT_OP_FWD, R, V, H, x, ldx, W_dev, ldw, grads ? e16 : nullptr, p.lde, xl, nullptr, status_dev, nullptr, 0, st);
         if (e != cudaSuccess) break;
         e = launch_pdl(k_ce_combine, dim3((unsigned)((R + 3) / 4)), dim3(256), 0, st, (const float2 *)stats, R, V, p.groups, labels,
-                       (const float *)zlabel, rowsum, row_loss_dev + r0, bad_labels_dev, x, ldx, H, xs);
+                       (const float *)zlabel, rowsum, row_loss_dev + r0, bad_labels_dev, x, ldx, H, xs, factor);
         if (e != cudaSuccess || !grads) continue;
-        e = launch_pdl(k_ce_rescale, dim3((unsigned)((p.lde + 2047) / 2048), (unsigned)((R + 7) / 8)), dim3(256), 0, st, e16, p.lde,
-                       (const float2 *)stats, R, V, labels, (const float *)zlabel, (const float2 *)rowsum);
+        e = launch_pdl(k_ce_rescale, dim3((unsigned)((p.lde + 16383) / 16384), (unsigned)R), dim3(256), 0, st, e16, p.lde,
+                       (const float *)factor, p.groups, V, labels, (const float *)zlabel, (const float2 *)rowsum);
         if (e == cudaSuccess && dx_dev) {
             xd.alpha = alpha;
             xd.max_split = kDxSplit;

@@ -126,6 +126,7 @@ struct ProductExtra {
     int acc_add = 0, acc_store = 0;
     const CeEpi *ce = nullptr;    // softmax epilogue (forward products)
     int max_split = 8;            // single-CTA kernel: most parts the contraction may be cut into
+    int split = 0;                // CTA-pair kernel: cut the contraction into this many parts, part by part (0: its own choice)
 };
 
 // Launchers (each returns a cudaError_t from the launch; all asynchronous on `st`).
