@@ -513,20 +513,23 @@ void mpt_lstm_destroy(mpt_lstm_ctx *ctx);
  * mean / rstd: float [rows]; the forward pass writes them for the backward pass, either may be null there.
  * nonfinite_flag (may be null): a uint32 that is OR-ed with 1 when an element of dgamma or dbeta is inf or NaN
  * (section 3.2).  Gradients are scaled by S if dy is; they are overwritten, not accumulated into.
+ * status_dev (may be null): one uint32 the caller has zeroed, receives a time-out code if a bounded wait runs out
+ * (results are then invalid).
  * workspace: mpt_layernorm_workspace_bytes, 16-byte aligned, owned by the caller and in use until the call's
  * stream work has completed (calls that may overlap need one each).  Results are run-to-run identical.
- * Rows that are 16-byte aligned (base pointers, and pitches that are multiples of 8) move in 16-byte pieces, others
- * element by element; any cols from 1 on is accepted.  Outputs must not overlap inputs (the same pointer is
+ * Rows that are 16-byte aligned (base pointers, and pitches that are multiples of 8) move by bulk copies and 16-byte
+ * stores, others element by element; rows of more than 12288 features are read more than once (by kernels that keep
+ * nothing of a row on chip).  cols from 1 to 2^30.  Outputs must not overlap inputs (the same pointer is
  * refused).  rows == 0: forward does nothing, backward writes zero dgamma and dbeta.  The stream must belong to
  * the current device (the launch fails otherwise: MPT_ERR_CUDA).  Bytes moved per element: 4 forward, 6 backward. */
 int mpt_layernorm_forward(int rows, int cols, const uint16_t *x_dev, int ldx, const uint16_t *gamma16_dev,
                           const uint16_t *beta16_dev, float eps, uint16_t *y_dev, int ldy, float *mean_dev, float *rstd_dev,
-                          void *cuda_stream);
+                          uint32_t *status_dev, void *cuda_stream);
 int mpt_layernorm_workspace_bytes(int rows, int cols, size_t *bytes_out);
 int mpt_layernorm_backward(int rows, int cols, const uint16_t *dy_dev, int lddy, const uint16_t *x_dev, int ldx,
                            const uint16_t *gamma16_dev, const float *mean_dev, const float *rstd_dev, uint16_t *dx_dev, int lddx,
-                           uint16_t *dgamma16_dev, uint16_t *dbeta16_dev, uint32_t *nonfinite_flag_dev, void *workspace_dev,
-                           size_t workspace_bytes, void *cuda_stream);
+                           uint16_t *dgamma16_dev, uint16_t *dbeta16_dev, uint32_t *nonfinite_flag_dev, uint32_t *status_dev,
+                           void *workspace_dev, size_t workspace_bytes, void *cuda_stream);
 
 /* Softmax cross-entropy forward and scaled backward (sections 3.2, 3.3), arithmetic
  * as in mpt_backward_scaled.  z_dev/dz_dev: FP16 [B, C] with pitches ldz/lddz

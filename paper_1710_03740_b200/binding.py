@@ -158,9 +158,9 @@ def lib() -> C.CDLL:
     L.mpt_lstm_cell_backward.argtypes = [i32, i32, vp, i32, vp, i32, vp, i32, vp, i32, vp, i32, vp, i32, vp, i32, vp]
     L.mpt_bias_grad.argtypes = [vp, sz, i32, i32, vp, vp, vp, vp]
     L.mpt_add_f16.argtypes = [vp, i32, vp, i32, vp, i32, i32, i32, vp]
-    L.mpt_layernorm_forward.argtypes = [i32, i32, vp, i32, vp, vp, f32, vp, i32, vp, vp, vp]
+    L.mpt_layernorm_forward.argtypes = [i32, i32, vp, i32, vp, vp, f32, vp, i32, vp, vp, vp, vp]
     L.mpt_layernorm_workspace_bytes.argtypes = [i32, i32, C.POINTER(sz)]
-    L.mpt_layernorm_backward.argtypes = [i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+    L.mpt_layernorm_backward.argtypes = [i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
     L.mpt_linear_ce_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i32, C.POINTER(sz)]
     L.mpt_linear_ce.argtypes = [i32, i32, i32, vp, i32, vp, i32, vp, f32, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
     L.mpt_distill_topk.argtypes = [vp, i32, i32, i32, vp, vp, i32, i32, f32, f32, vp, i32, vp, vp, vp, vp]
@@ -564,9 +564,10 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
-def mpt_layernorm_forward(rows, cols, x, ldx, gamma16, beta16, eps, y, ldy, mean=None, rstd=None, stream=None):
-    st = _stream_of(stream, ((x, 2), (gamma16, 2), (beta16, 2), (y, 2), (mean, 4), (rstd, 4)))
-    _check(lib().mpt_layernorm_forward(rows, cols, _at(x), ldx, _at(gamma16), _at(beta16), eps, _at(y), ldy, _at(mean), _at(rstd), st))
+def mpt_layernorm_forward(rows, cols, x, ldx, gamma16, beta16, eps, y, ldy, mean=None, rstd=None, status=None, stream=None):
+    st = _stream_of(stream, ((x, 2), (gamma16, 2), (beta16, 2), (y, 2), (mean, 4), (rstd, 4), (status, 4)))
+    _check(lib().mpt_layernorm_forward(rows, cols, _at(x), ldx, _at(gamma16), _at(beta16), eps, _at(y), ldy, _at(mean), _at(rstd), _at(status),
+                                       st))
 
 
 def mpt_layernorm_workspace_bytes(rows, cols) -> int:
@@ -576,12 +577,13 @@ def mpt_layernorm_workspace_bytes(rows, cols) -> int:
 
 
 def mpt_layernorm_backward(rows, cols, dy, lddy, x, ldx, gamma16, mean, rstd, dx, lddx, dgamma16, dbeta16, workspace,
-                           nonfinite_flag=None, stream=None):
+                           nonfinite_flag=None, status=None, stream=None):
     """workspace: a uint8 tensor of at least mpt_layernorm_workspace_bytes(rows, cols)."""
     st = _stream_of(stream, ((dy, 2), (x, 2), (gamma16, 2), (mean, 4), (rstd, 4), (dx, 2), (dgamma16, 2), (dbeta16, 2),
-                             (nonfinite_flag, 4), (workspace, 1)))
+                             (nonfinite_flag, 4), (status, 4), (workspace, 1)))
     _check(lib().mpt_layernorm_backward(rows, cols, _at(dy), lddy, _at(x), ldx, _at(gamma16), _at(mean), _at(rstd), _at(dx), lddx,
-                                        _at(dgamma16), _at(dbeta16), _at(nonfinite_flag), _at(workspace), workspace.numel(), st))
+                                        _at(dgamma16), _at(dbeta16), _at(nonfinite_flag), _at(status), _at(workspace),
+                                        workspace.numel(), st))
 
 
 # ------------------------------------------------------------ vocabulary head with its loss

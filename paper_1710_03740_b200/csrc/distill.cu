@@ -467,13 +467,28 @@ struct Cta {
             dead = true;
         }
     }
+    // Whole vectors among [f, f + n) of this warp's part as the copy of row i takes them.  A last, partial vector comes with
+    // what the pitch leaves behind it (mend() replaces that), but for the matrix's last row, whose memory may end with it.
+    __device__ __forceinline__ int copied(int i, int f, int n) const
+    {
+        return row_of(i) == p.B - 1 ? min(n, p.C / 8 - (v0 + f)) : n;
+    }
+    // Logits behind the last class become -inf (nothing to do unless the part ends in a partial vector).
+    __device__ __forceinline__ void mend(int i, int s, int f, int n)
+    {
+        if (BULK && (v0 + f + n) * 8 > p.C) {
+            if (copied(i, f, n) == n && lane < 8 && (v0 + f + n - 1) * 8 + lane >= p.C)
+                ((uint16_t *)(buf + s * p.per + n - 1))[lane] = (uint16_t)kNegInf16;
+            __syncwarp();
+        }
+    }
     // Requests vectors [f, f + n) of this warp's part of row i into buffer s (the caller knows that it is free).
     __device__ __forceinline__ void request(int i, int s, int f, int n, uint64_t policy)
     {
         const uint16_t *src = p.z + (size_t)row_of(i) * p.ldz + (size_t)(v0 + f) * 8;
         uint4 *dst = buf + s * p.per;
         if (BULK) {
-            const int whole = min(n, p.C / 8 - (v0 + f));             // n - 1 where the part ends in a partial vector
+            const int whole = copied(i, f, n);
             if (lane == 0) {                                          // each use of a buffer completes one phase of its barrier
                 if (whole > 0) bulk_in(smem_u32(dst), src, (uint32_t)whole * 16u, bar0 + 8u * (uint32_t)s, policy);
                 else mbar_arrive(bar0 + 8u * (uint32_t)s);
@@ -644,6 +659,7 @@ __global__ void __launch_bounds__((kMaxWarps + kTeachers) * 32, 1) k_distill(con
         float m = -INFINITY, b = 0.0f, s = 0.0f;
         if (nv > 0) {
             c.arrived(s_use, parity);
+            c.mend(i, s_use, 0, nv);
             uint4 x[R];
             __half2 mx = __half2half2(__ushort_as_half((unsigned short)kNegInf16));
 #pragma unroll
@@ -753,6 +769,7 @@ __global__ void __launch_bounds__((kMaxWarps + kTeachers) * 32, 1) k_distill_str
         for (int ch = 0; ch < nch; ch++) {
             ask();
             c.arrived(s_use, parity);
+            c.mend(i, s_use, ch * per, min(per, nv - ch * per));
             run_vectors(r, c.buf + s_use * per, min(per, nv - ch * per), p.k);
             __syncwarp();
             consumed();
@@ -768,6 +785,7 @@ __global__ void __launch_bounds__((kMaxWarps + kTeachers) * 32, 1) k_distill_str
             for (int ch = 0; ch < nch; ch++) {
                 ask();
                 c.arrived(s_use, parity);
+                c.mend(i, s_use, ch * per, min(per, nv - ch * per));
                 const int n = min(per, nv - ch * per), first = (c.v0 + ch * per) * 8;
                 const uint4 *v = c.buf + s_use * per;
                 uint16_t *dst = c.out(i) + ch * per * 8;

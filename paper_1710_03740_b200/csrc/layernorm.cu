@@ -7,14 +7,19 @@
 //             dgamma = rn16(sum over rows of dy * h) ;  dbeta = rn16(sum over rows of dy)
 //
 // Bound: HBM.  Forward reads x and writes y (4 bytes an element), backward reads dy and x and writes dx (6).
-// A row lives in the registers of one warp (up to 1024 features) or of one CTA, so everything is read once;
-// the variance is a second pass over those registers (sum of squared deviations), not a difference of sums.
-// The backward pass adds dy*h and dy into per-thread FP32 column sums while the rows stream by, leaves one
-// partial row of them per CTA in the workspace and adds those in a second kernel in a fixed order: results are
-// run-to-run identical, nothing is added atomically.  The partial sums are at most 296 rows whatever the batch.
+// Up to 1024 features belong to one warp, longer rows (up to 12288 features) to as many warps of a CTA as that takes;
+// a warp keeps its features for all rows it works on, so the column sums of the parameter gradients stay in its registers.  Every warp is a pipeline of its own: its part of the next rows arrives in shared
+// memory by bulk copies while the present row is in registers (with all SMs' copies queued at the memory a load takes a
+// few microseconds, longer than a row), results leave by 16-byte stores.  The warps of a long row exchange their
+// sums through shared memory and a named barrier.  The variance is a second pass over the registers (sum of squared
+// deviations), not a difference of sums.
+// The backward pass adds dy*h and dy into per-lane FP32 column sums, leaves one partial row of them per CTA in the
+// workspace and adds those in a second kernel in a fixed order: results are run-to-run identical, nothing is added
+// atomically.  The partial sums are at most 148 rows whatever the batch.
 #include <math.h>
 
 #include "mpt_common.cuh"
+#include "tc_ptx.cuh"
 
 namespace mpt {
 namespace {
@@ -39,6 +44,67 @@ __device__ __forceinline__ uint4 pack8(const float (&f)[8])
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
+
+// Two FP32 values in one 64-bit register: add, mul and fma of both (each rounded as the scalar operation) in one
+// instruction, which halves the issue slots that these kernels would otherwise run out of before HBM does.
+typedef unsigned long long f2;
+__device__ __forceinline__ f2 pair(float a, float b)
+{
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 halves(f2 v)
+{
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ f2 add2(f2 a, f2 b)
+{
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b)
+{
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
+{
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ float sum2(f2 v)
+{
+    const float2 t = halves(v);
+    return t.x + t.y;
+}
+__device__ __forceinline__ void widen8(const uint4 v, f2 (&f)[4])
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+        const float2 t = __half22float2(*(const __half2 *)&w[q]);
+        f[q] = pair(t.x, t.y);
+    }
+}
+__device__ __forceinline__ uint4 round8(const f2 (&f)[4])
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+        const float2 t = halves(f[q]);
+        const __half2 h = __floats2half2_rn(t.x, t.y);
+        w[q] = *(const uint32_t *)&h;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+struct Whole { static constexpr bool value = true; };      // a warp's part is 32 R whole vectors: no element needs a check
+struct Ragged { static constexpr bool value = false; };
 
 // Eight neighbouring FP16 values of a row, zeros from `cols` on.  VEC: the row starts on a 16-byte boundary.
 // STREAM: data that is used once (evict first); the scale and shift vectors are read by every row instead and
@@ -95,8 +161,148 @@ __device__ __forceinline__ void cta_sum2(float &a, float &b, float2 *red)
     b = warp_sum(r.y);
 }
 
+// The work of one warp: features [8 v0, 8 (v0 + nv)) of the rows first, first + stride, ... (n of them), and the ring of
+// buffers through which NIN input matrices arrive.
+constexpr int kLnWarps = 12;          // warps of a CTA
+constexpr int kLnMaxRowWarps = 12;    // warps a row may take: 12288 features
+constexpr int kLnBuffers = 4;         // even: what follows their mbarriers is 16-byte aligned
+
+template <int R, int NIN, bool BULK>
+struct LnWarp {
+    int warp, lane, w, g, nw, v0, nv, c8, rows, cols, first, stride, n;
+    const uint16_t *src[NIN];
+    size_t ld[NIN];
+    uint4 *buf;
+    uint32_t bar;
+    int s_ask = 0, s_use = 0;
+    uint32_t parity = 0;
+    volatile uint32_t *abort_flag;
+    uint32_t *status;
+    bool dead = false;
+
+    static constexpr int kSlot = NIN * R * 32;      // vectors of a buffer
+
+    // shared memory: buffers [warps][kLnBuffers][NIN][32 R] of 16 bytes | mbarriers [warps][kLnBuffers] | the caller's
+    __device__ __forceinline__ LnWarp(uint8_t *smem, int row_warps, int rows_, int cols_, volatile uint32_t *abort, uint32_t *status_)
+    {
+        warp = threadIdx.x >> 5;
+        lane = threadIdx.x & 31;
+        nw = row_warps;
+        const int warps = (int)blockDim.x >> 5, groups = warps / nw;
+        g = warp / nw;
+        w = warp - g * nw;
+        rows = rows_;
+        cols = cols_;
+        c8 = (cols + 7) / 8;
+        v0 = w * 32 * R;
+        nv = min(c8 - v0, 32 * R);
+        first = (int)blockIdx.x * groups + g;
+        stride = (int)gridDim.x * groups;
+        n = first < rows ? (rows - 1 - first) / stride + 1 : 0;
+        buf = (uint4 *)smem + (size_t)warp * kLnBuffers * kSlot;
+        bar = smem_u32(smem + (size_t)warps * kLnBuffers * kSlot * 16) + 8u * (uint32_t)(warp * kLnBuffers);
+        abort_flag = abort;
+        status = status_;
+        if (lane == 0)
+            for (int s = 0; s < kLnBuffers; s++) mbar_init(bar + 8u * (uint32_t)s, 1);
+        if (threadIdx.x == 0) *abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
+    }
+    __device__ __forceinline__ int row_of(int i) const { return first + i * stride; }
+    // Row i into the next buffer (which is free).  A last, partial vector comes whole with what the pitch leaves behind it
+    // (take() clears that), but for the matrix's last row, whose memory may end with it: there element by element.
+    __device__ __forceinline__ void request(int i)
+    {
+        if (i >= n) return;
+        uint4 *dst = buf + s_ask * kSlot;
+        const int whole = row_of(i) == rows - 1 ? min(nv, cols / 8 - v0) : nv;
+        const uint32_t b = bar + 8u * (uint32_t)s_ask;
+        if (BULK && lane == 0) {
+            if (whole > 0) mbar_arrive_expect_tx(b, (uint32_t)(NIN * whole) * 16u);
+            else mbar_arrive(b);
+        }
+#pragma unroll
+        for (int k = 0; k < NIN; k++) {
+            const uint16_t *from = src[k] + (size_t)row_of(i) * ld[k] + (size_t)v0 * 8;
+            uint4 *to = dst + k * R * 32;
+            if (BULK) {
+                if (lane == 0 && whole > 0)
+                    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                 ::"r"(smem_u32(to)), "l"(from), "r"((uint32_t)whole * 16u), "r"(b) : "memory");
+                if (whole < nv && lane < 8) ((uint16_t *)(to + whole))[lane] = (v0 + whole) * 8 + lane < cols ? from[whole * 8 + lane] : (uint16_t)0;
+            } else {
+                for (int e = lane; e < nv * 8; e += 32) ((uint16_t *)to)[e] = v0 * 8 + e < cols ? from[e] : (uint16_t)0;
+            }
+        }
+        __syncwarp();
+        s_ask = s_ask + 1 == kLnBuffers ? 0 : s_ask + 1;
+    }
+    // Keeps the first `left` of eight values, zeros behind them.
+    __device__ __forceinline__ static void clear_behind(uint4 &v, int left)
+    {
+        v.x = left >= 2 ? v.x : (left == 1 ? v.x & 0xFFFFu : 0u);
+        v.y = left >= 4 ? v.y : (left == 3 ? v.y & 0xFFFFu : 0u);
+        v.z = left >= 6 ? v.z : (left == 5 ? v.z & 0xFFFFu : 0u);
+        v.w = left >= 8 ? v.w : (left == 7 ? v.w & 0xFFFFu : 0u);
+    }
+    // The next row into registers (zeros from the last feature on).
+    template <bool WHOLE>
+    __device__ __forceinline__ void take(uint4 (&x)[NIN][R])
+    {
+        if (BULK && !mbar_try_wait(bar + 8u * (uint32_t)s_use, parity) && !mbar_wait(bar + 8u * (uint32_t)s_use, parity, abort_flag)) {
+            // all later waits of the CTA end at once; what is computed from here on is not valid
+            if (status && !*abort_flag) atomicCAS(status, 0u, (uint32_t)KERR_WAIT_FULL | 0x40u | ((uint32_t)blockIdx.x << 8));
+            *abort_flag = 1u;
+            dead = true;
+        }
+        const uint4 *from = buf + s_use * kSlot;
+#pragma unroll
+        for (int k = 0; k < NIN; k++) {
+#pragma unroll
+            for (int u = 0; u < R; u++) {
+                const int j = lane + 32 * u;
+                x[k][u] = WHOLE || j < nv ? from[k * R * 32 + j] : make_uint4(0u, 0u, 0u, 0u);
+                if (!WHOLE && !whole(u)) clear_behind(x[k][u], cols - (v0 + j) * 8);
+            }
+        }
+        __syncwarp();
+        if (++s_use == kLnBuffers) {
+            s_use = 0;
+            parity ^= 1u;
+        }
+    }
+    // Sum over the row's warps, in warp order; `red`: 16 words of this group, zero from nw on.
+    __device__ __forceinline__ float row_sum(float v, float *red) const
+    {
+        v = warp_sum(v);
+        if (nw == 1) return v;
+        if (lane == 0) red[w] = v;
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + g), "r"(nw * 32) : "memory");
+        float s = 0.0f;
+#pragma unroll
+        for (int q = 0; q < kLnMaxRowWarps / 4; q++) {
+            const float4 t = ((const float4 *)red)[q];
+            s += (t.x + t.y) + (t.z + t.w);
+        }
+        return s;
+    }
+    // After a wait that ran out: copies still on their way get a bounded time to land before the CTA's memory is used otherwise.
+    __device__ __forceinline__ void settle() const
+    {
+        if (dead) {
+            const unsigned long long t0 = global_ns();
+            while (global_ns() - t0 < 1000000ull) {}
+        }
+        __syncthreads();
+    }
+    // whether the warp's vectors 32 u ... 32 u + 31 are all whole (the same for all lanes)
+    __device__ __forceinline__ bool whole(int u) const { return BULK && (v0 + 32 * (u + 1)) * 8 <= cols; }
+};
+
 struct LnFwd {
-    int rows, cols;
+    int rows, cols, row_warps;
     const uint16_t *x;
     size_t ldx;
     const uint16_t *gamma, *beta;      // beta may be null
@@ -104,77 +310,91 @@ struct LnFwd {
     uint16_t *y;
     size_t ldy;
     float *mean, *rstd;                // may be null
+    uint32_t *status;                  // may be null
 };
 
-// One row per warp (WARP) or per CTA; thread t of the group holds the vectors t, t + T, ... (at most VPT).
-// MAXT threads at most; rows of one CTA are kept to 384 threads where they fit (12288 features), so that four
-// CTAs share an SM and one row's loads run under another's reductions.
-template <int VPT, bool VEC, bool WARP, int MAXT>
-__global__ void __launch_bounds__(MAXT, MAXT == 384 ? 4 : 1) k_ln_fwd(const LnFwd p)
+template <int R, bool BULK>
+__global__ void __launch_bounds__(kLnWarps * 32, 2) k_ln_fwd(const LnFwd p)
 {
     pdl_trigger();
     pdl_wait();
-    __shared__ float red[2][32];
-    const int T = WARP ? 32 : blockDim.x, t = WARP ? threadIdx.x & 31 : threadIdx.x;
-    const int per_cta = WARP ? blockDim.x >> 5 : 1;
-    const float n = (float)p.cols;
-    for (int row = blockIdx.x * per_cta + (WARP ? threadIdx.x >> 5 : 0); row < p.rows; row += gridDim.x * per_cta) {
-        const uint16_t *xr = p.x + (size_t)row * p.ldx;
-        uint4 v[VPT];
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(16) float red[kLnWarps][2][16];
+    __shared__ uint32_t abort_word;
+    for (int i = threadIdx.x; i < kLnWarps * 32; i += blockDim.x) (&red[0][0][0])[i] = 0.0f;
+    LnWarp<R, 1, BULK> c(smem, p.row_warps, p.rows, p.cols, &abort_word, p.status);
+    c.src[0] = p.x;
+    c.ld[0] = p.ldx;
+    for (int i = 0; i < kLnBuffers; i++) c.request(i);
+    const float inv_n = __fdiv_rn(1.0f, (float)p.cols);
+    const int col0 = (c.v0 + c.lane) * 8;
+    auto rows = [&](auto whole) {
+        constexpr bool W = decltype(whole)::value;
+        for (int i = 0; i < c.n; i++) {
+            uint4 x[1][R];
+            c.template take<W>(x);
+            c.request(i + kLnBuffers);
+            f2 f[R][4];
+            f2 s = pair(0.0f, 0.0f);
 #pragma unroll
-        for (int u = 0; u < VPT; u++) {
-            const int col = (t + u * T) * 8;
-            v[u] = col < p.cols ? load8<VEC, true>(xr, col, p.cols) : make_uint4(0u, 0u, 0u, 0u);
-        }
-        float s = 0.0f;
+            for (int u = 0; u < R; u++) {
+                widen8(x[0][u], f[u]);
+                s = add2(s, add2(add2(f[u][0], f[u][1]), add2(f[u][2], f[u][3])));
+            }
+            const float mean = c.row_sum(sum2(s), red[c.g][0]) * inv_n;
+            const f2 minus = pair(-mean, -mean);
+            f2 q0 = pair(0.0f, 0.0f), q1 = q0;
 #pragma unroll
-        for (int u = 0; u < VPT; u++) {
-            float f[8];
-            unpack8(v[u], f);
-            s += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
-        }
-        const float mean = __fdiv_rn(WARP ? warp_sum(s) : cta_sum(s, red[0]), n);
-        float d2 = 0.0f;
+            for (int u = 0; u < R; u++) {
 #pragma unroll
-        for (int u = 0; u < VPT; u++) {
-            const int col = (t + u * T) * 8;
-            float f[8];
-            unpack8(v[u], f);
-            if (col + 8 <= p.cols) {
+                for (int e = 0; e < 4; e++) f[u][e] = add2(f[u][e], minus);
+                if (!W && !c.whole(u)) {           // what lies behind the last feature must not count: deviation zero
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    const float d = f[e] - mean;
-                    d2 = fmaf(d, d, d2);
+                    for (int e = 0; e < 4; e++) {
+                        const int col = col0 + 256 * u + 2 * e;
+                        const float2 d = halves(f[u][e]);
+                        f[u][e] = pair(col < p.cols ? d.x : 0.0f, col + 1 < p.cols ? d.y : 0.0f);
+                    }
                 }
-            } else if (col < p.cols) {
 #pragma unroll
-                for (int e = 0; e < 7; e++) {
-                    const float d = f[e] - mean;
-                    if (col + e < p.cols) d2 = fmaf(d, d, d2);
+                for (int e = 0; e < 4; e += 2) {
+                    q0 = fma2(f[u][e], f[u][e], q0);
+                    q1 = fma2(f[u][e + 1], f[u][e + 1], q1);
+                }
+            }
+            const float var = c.row_sum(sum2(add2(q0, q1)), red[c.g][1]) * inv_n;
+            const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(var + p.eps));
+            const int row = c.row_of(i);
+            if (c.w == 0 && c.lane == 0) {
+                if (p.mean) p.mean[row] = mean;
+                if (p.rstd) p.rstd[row] = rstd;
+            }
+            uint16_t *yr = p.y + (size_t)row * p.ldy + col0;
+            const f2 r2 = pair(rstd, rstd);
+#pragma unroll
+            for (int u = 0; u < R; u++) {
+                const int col = col0 + 256 * u;
+                const bool whole_u = W || c.whole(u);
+                if (whole_u || col < p.cols) {
+                    f2 g[4], b[4];
+                    if (whole_u) {                // these two stay in L1
+                        widen8(__ldg((const uint4 *)(p.gamma + col)), g);
+                        widen8(p.beta ? __ldg((const uint4 *)(p.beta + col)) : make_uint4(0u, 0u, 0u, 0u), b);
+                    } else {
+                        widen8(load8<BULK, false>(p.gamma, col, p.cols), g);
+                        widen8(p.beta ? load8<BULK, false>(p.beta, col, p.cols) : make_uint4(0u, 0u, 0u, 0u), b);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; e++) f[u][e] = fma2(mul2(f[u][e], r2), g[e], b[e]);
+                    if (whole_u) __stcs((uint4 *)(yr + 256 * u), round8(f[u]));
+                    else store8<BULK>(yr - col0, col, p.cols, round8(f[u]));
                 }
             }
         }
-        const float var = __fdiv_rn(WARP ? warp_sum(d2) : cta_sum(d2, red[1]), n);
-        const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(var + p.eps));
-        if (t == 0) {
-            if (p.mean) p.mean[row] = mean;
-            if (p.rstd) p.rstd[row] = rstd;
-        }
-        uint16_t *yr = p.y + (size_t)row * p.ldy;
-#pragma unroll
-        for (int u = 0; u < VPT; u++) {
-            const int col = (t + u * T) * 8;
-            if (col < p.cols) {
-                float f[8], g[8], b[8] = {};
-                unpack8(v[u], f);
-                unpack8(load8<VEC, false>(p.gamma, col, p.cols), g);
-                if (p.beta) unpack8(load8<VEC, false>(p.beta, col, p.cols), b);
-#pragma unroll
-                for (int e = 0; e < 8; e++) f[e] = fmaf((f[e] - mean) * rstd, g[e], b[e]);
-                store8<VEC>(yr, col, p.cols, pack8(f));
-            }
-        }
-    }
+    };
+    if (c.whole(R - 1)) rows(Whole{});
+    else rows(Ragged{});
+    c.settle();
 }
 
 // Rows too long for one CTA's registers: three passes over the row (the second and third hit L2).
@@ -224,7 +444,7 @@ __global__ void __launch_bounds__(1024) k_ln_fwd_long(const LnFwd p)
 }
 
 struct LnBwd {
-    int rows, cols;
+    int rows, cols, row_warps;
     const uint16_t *dy;
     size_t lddy;
     const uint16_t *x;
@@ -235,127 +455,146 @@ struct LnBwd {
     size_t lddx;
     float *parts;                      // [2][gridDim.x][colp]: partial dgamma, then partial dbeta
     int colp;
+    uint32_t *status;                  // may be null
 };
 
-// One row per warp (WARP, 8 warps) or per CTA.  The next row's loads are issued before the reduction of the
-// present one.
-template <int VPT, bool VEC, bool WARP>
-__global__ void __launch_bounds__(WARP ? 256 : 768) k_ln_bwd(const LnBwd p)
+template <int R, bool BULK>
+__global__ void __launch_bounds__(kLnWarps * 32, 1) k_ln_bwd(const LnBwd p)
 {
     pdl_trigger();
     pdl_wait();
-    extern __shared__ float cols_smem[];            // WARP: [8 warps][VPT * 256]
-    __shared__ float2 red[2][32];
-    const int T = WARP ? 32 : blockDim.x, t = WARP ? threadIdx.x & 31 : threadIdx.x;
-    const int per_cta = WARP ? 8 : 1, warp = threadIdx.x >> 5;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(16) float red[kLnWarps][2][2][16];
+    __shared__ uint32_t abort_word;
+    for (int i = threadIdx.x; i < kLnWarps * 64; i += blockDim.x) (&red[0][0][0][0])[i] = 0.0f;
+    LnWarp<R, 2, BULK> c(smem, p.row_warps, p.rows, p.cols, &abort_word, p.status);
+    c.src[0] = p.x;
+    c.ld[0] = p.ldx;
+    c.src[1] = p.dy;
+    c.ld[1] = p.lddy;
+    for (int i = 0; i < kLnBuffers; i++) c.request(i);
+    const int col0 = (c.v0 + c.lane) * 8;
+    // gamma in shared memory, behind the mbarriers: zeros from the last feature on
+    uint4 *gamma = (uint4 *)(smem + (size_t)(blockDim.x >> 5) * kLnBuffers * (LnWarp<R, 2, BULK>::kSlot * 16 + 8));
+    for (int j = threadIdx.x; j < c.nw * 32 * R; j += blockDim.x)
+        gamma[j] = j * 8 < p.cols ? load8<BULK, false>(p.gamma, j * 8, p.cols) : make_uint4(0u, 0u, 0u, 0u);
+    __syncthreads();
+    gamma += c.v0 + c.lane;
+    f2 ag[R][4], ab[R][4];
+#pragma unroll
+    for (int u = 0; u < R; u++) {
+#pragma unroll
+        for (int e = 0; e < 4; e++) ag[u][e] = ab[u][e] = pair(0.0f, 0.0f);
+    }
     const float inv_n = __fdiv_rn(1.0f, (float)p.cols);
-    float ag[VPT][8], ab[VPT][8];
-    uint4 gm[VPT];
-#pragma unroll
-    for (int u = 0; u < VPT; u++) {
-        const int col = (t + u * T) * 8;
-        gm[u] = col < p.cols ? load8<VEC, false>(p.gamma, col, p.cols) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-        for (int e = 0; e < 8; e++) ag[u][e] = ab[u][e] = 0.0f;
-    }
-    const int first = blockIdx.x * per_cta + (WARP ? warp : 0), stride = gridDim.x * per_cta;
-    uint4 nx[VPT], nd[VPT];
-    float nmean = 0.0f, nrstd = 0.0f;
-    auto fetch = [&](int row) {
-        const uint16_t *xr = p.x + (size_t)row * p.ldx, *dr = p.dy + (size_t)row * p.lddy;
-#pragma unroll
-        for (int u = 0; u < VPT; u++) {
-            const int col = (t + u * T) * 8;
-            nx[u] = nd[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (col < p.cols) {
-                nx[u] = load8<VEC, true>(xr, col, p.cols);
-                nd[u] = load8<VEC, true>(dr, col, p.cols);
+    auto rows = [&](auto whole) {
+        constexpr bool W = decltype(whole)::value;
+        // the statistics of 32 rows at a time, one per lane, asked for 32 rows ahead
+        float mean_next = 0.0f, rstd_next = 0.0f, mean32 = 0.0f, rstd32 = 0.0f;
+        auto ask_stats = [&](int i) {
+            if (i + c.lane < c.n) {
+                mean_next = p.mean[c.row_of(i + c.lane)];
+                rstd_next = p.rstd[c.row_of(i + c.lane)];
             }
-        }
-        nmean = p.mean[row];
-        nrstd = p.rstd[row];
-    };
-    if (first < p.rows) fetch(first);
-    int flip = 0;
-    for (int row = first; row < p.rows; row += stride, flip ^= 1) {
-        uint4 vx[VPT], vd[VPT];
-#pragma unroll
-        for (int u = 0; u < VPT; u++) { vx[u] = nx[u]; vd[u] = nd[u]; }
-        const float mean = nmean, rstd = nrstd;
-        if (row + stride < p.rows) fetch(row + stride);
-        float c1 = 0.0f, c2 = 0.0f;
-#pragma unroll
-        for (int u = 0; u < VPT; u++) {
-            float x[8], d[8], g[8];
-            unpack8(vx[u], x);
-            unpack8(vd[u], d);
-            unpack8(gm[u], g);
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const float h = (x[e] - mean) * rstd, gy = d[e] * g[e];
-                c1 += gy;
-                c2 = fmaf(gy, h, c2);
-                ag[u][e] = fmaf(d[e], h, ag[u][e]);
-                ab[u][e] += d[e];
+        };
+        ask_stats(0);
+        for (int i = 0; i < c.n; i++) {
+            if ((i & 31) == 0) {
+                mean32 = mean_next;
+                rstd32 = rstd_next;
+                ask_stats(i + 32);
             }
-        }
-        if (WARP) {
-            c1 = warp_sum(c1);
-            c2 = warp_sum(c2);
-        } else {
-            cta_sum2(c1, c2, red[flip]);
-        }
-        c1 *= inv_n;
-        c2 *= inv_n;
-        uint16_t *o = p.dx + (size_t)row * p.lddx;
+            const float mean = __shfl_sync(0xFFFFFFFFu, mean32, i & 31), rstd = __shfl_sync(0xFFFFFFFFu, rstd32, i & 31);
+            const f2 minus = pair(-mean, -mean), r2 = pair(rstd, rstd);
+            uint4 v[2][R];
+            c.template take<W>(v);
+            c.request(i + kLnBuffers);
+            f2 h[R][4], gy[R][4];
+            f2 s1 = pair(0.0f, 0.0f), s2 = s1;
 #pragma unroll
-        for (int u = 0; u < VPT; u++) {
-            const int col = (t + u * T) * 8;
-            if (col < p.cols) {
-                float x[8], d[8], g[8];
-                unpack8(vx[u], x);
-                unpack8(vd[u], d);
-                unpack8(gm[u], g);
+            for (int u = 0; u < R; u++) {
+                f2 d[4], g[4];
+                widen8(v[0][u], h[u]);
+                widen8(v[1][u], d);
+                widen8(gamma[32 * u], g);
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    const float h = (x[e] - mean) * rstd;
-                    d[e] = rstd * (fmaf(d[e], g[e], -c1) - h * c2);
+                for (int e = 0; e < 4; e++) {
+                    h[u][e] = mul2(add2(h[u][e], minus), r2);
+                    gy[u][e] = mul2(d[e], g[e]);
+                    s1 = add2(s1, gy[u][e]);
+                    s2 = fma2(gy[u][e], h[u][e], s2);
+                    ag[u][e] = fma2(d[e], h[u][e], ag[u][e]);
+                    ab[u][e] = add2(ab[u][e], d[e]);
                 }
-                store8<VEC>(o, col, p.cols, pack8(d));
+            }
+            float c1 = warp_sum(sum2(s1)), c2 = warp_sum(sum2(s2));
+            if (c.nw > 1) {
+                float (*r)[16] = red[c.g][i & 1];            // the two are a barrier apart
+                if (c.lane == 0) {
+                    r[0][c.w] = c1;
+                    r[1][c.w] = c2;
+                }
+                asm volatile("bar.sync %0, %1;" ::"r"(1 + c.g), "r"(c.nw * 32) : "memory");
+                c1 = c2 = 0.0f;
+#pragma unroll
+                for (int q = 0; q < kLnMaxRowWarps / 4; q++) {
+                    const float4 a = ((const float4 *)r[0])[q], b = ((const float4 *)r[1])[q];
+                    c1 += (a.x + a.y) + (a.z + a.w);
+                    c2 += (b.x + b.y) + (b.z + b.w);
+                }
+            }
+            const float m1 = -rstd * (c1 * inv_n), m2 = -rstd * (c2 * inv_n);
+            const f2 k1 = pair(m1, m1), k2 = pair(m2, m2);
+            uint16_t *o = p.dx + (size_t)c.row_of(i) * p.lddx + col0;
+#pragma unroll
+            for (int u = 0; u < R; u++) {
+                const bool whole_u = W || c.whole(u);
+                if (whole_u || col0 + 256 * u < p.cols) {
+#pragma unroll
+                    for (int e = 0; e < 4; e++) gy[u][e] = fma2(gy[u][e], r2, fma2(h[u][e], k2, k1));
+                    if (whole_u) __stcs((uint4 *)(o + 256 * u), round8(gy[u]));
+                    else store8<BULK>(o - col0, col0 + 256 * u, p.cols, round8(gy[u]));
+                }
             }
         }
-    }
-    // the CTA's column sums: for rows held by warps, the eight warps' sums are added in warp order
+    };
+    if (c.whole(R - 1)) rows(Whole{});
+    else rows(Ragged{});
+    c.settle();
+    // the CTA's column sums; where several groups of warps hold the same features, added in group order
     float *pg = p.parts + (size_t)blockIdx.x * p.colp, *pb = pg + (size_t)gridDim.x * p.colp;
-    if (WARP) {
+    const int groups = (int)(blockDim.x >> 5) / c.nw;
+    if (groups > 1) {
+        float *sums = (float *)smem;                     // [groups][nw * 256 R]: the buffers are not in use any more
+        const int width = c.nw * 256 * R;
 #pragma unroll
         for (int which = 0; which < 2; which++) {
             __syncthreads();
 #pragma unroll
-            for (int u = 0; u < VPT; u++) {
-                float4 *s = (float4 *)(cols_smem + warp * (VPT * 256) + (t + u * 32) * 8);
-                float (&a)[8] = which ? ab[u] : ag[u];
-                s[0] = make_float4(a[0], a[1], a[2], a[3]);
-                s[1] = make_float4(a[4], a[5], a[6], a[7]);
+            for (int u = 0; u < R; u++) {
+                float4 *s = (float4 *)(sums + c.g * width + (c.v0 + c.lane + 32 * u) * 8);
+                f2 (&a)[4] = which ? ab[u] : ag[u];
+                const float2 a0 = halves(a[0]), a1 = halves(a[1]), a2 = halves(a[2]), a3 = halves(a[3]);
+                s[0] = make_float4(a0.x, a0.y, a1.x, a1.y);
+                s[1] = make_float4(a2.x, a2.y, a3.x, a3.y);
             }
             __syncthreads();
-            for (int c = threadIdx.x; c < p.cols; c += 256) {
-                float s = cols_smem[c];
-#pragma unroll
-                for (int w = 1; w < 8; w++) s += cols_smem[w * (VPT * 256) + c];
-                (which ? pb : pg)[c] = s;
+            for (int col = threadIdx.x; col < p.cols; col += blockDim.x) {
+                float s = sums[col];
+                for (int k = 1; k < groups; k++) s += sums[k * width + col];
+                (which ? pb : pg)[col] = s;
             }
         }
     } else {
 #pragma unroll
-        for (int u = 0; u < VPT; u++) {
-            const int col = (t + u * T) * 8;
+        for (int u = 0; u < R; u++) {
+            const int col = (c.v0 + c.lane + 32 * u) * 8;
             if (col < p.cols) {                    // colp is a multiple of 8: a started vector is whole
-                float4 *s = (float4 *)(pg + col), *b = (float4 *)(pb + col);
-                s[0] = make_float4(ag[u][0], ag[u][1], ag[u][2], ag[u][3]);
-                s[1] = make_float4(ag[u][4], ag[u][5], ag[u][6], ag[u][7]);
-                b[0] = make_float4(ab[u][0], ab[u][1], ab[u][2], ab[u][3]);
-                b[1] = make_float4(ab[u][4], ab[u][5], ab[u][6], ab[u][7]);
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    *(float2 *)(pg + col + 2 * e) = halves(ag[u][e]);
+                    *(float2 *)(pb + col + 2 * e) = halves(ab[u][e]);
+                }
             }
         }
     }
@@ -461,50 +700,68 @@ __global__ void __launch_bounds__(256) k_ln_param_grad(const float *__restrict__
     }
 }
 
-constexpr int kLnMaxParts = 296;      // partial rows of the column sums: at most two CTAs on each of the 148 SMs
-
+constexpr int kLnMaxParts = 148;      // partial rows of the column sums: one CTA on each SM
 constexpr int kLnMaxCols = 1 << 30;   // column indexes stay far inside 32 bits
 
 int ln_colp(int cols) { return (cols + 7) / 8 * 8; }
 int ln_parts(int rows) { return rows < kLnMaxParts ? rows : kLnMaxParts; }
 
-template <int VPT, bool WARP, int MAXT>
-cudaError_t run_fwd(const LnFwd &p, bool vec, int grid, int threads, cudaStream_t st)
+// How rows of c8 vectors are laid over warps: R vectors a lane, row_warps warps a row, groups of them in a CTA (fewer
+// where there are not enough rows for all SMs), and the grid for `per_sm` CTAs of kLnWarps warps on an SM.
+struct LnShape {
+    int R, row_warps, groups, grid;
+};
+LnShape ln_shape(int rows, int c8, int per_sm)
 {
-    if (vec) MPT_LAUNCH((k_ln_fwd<VPT, true, WARP, MAXT>), dim3((unsigned)grid), dim3((unsigned)threads), 0, st, p);
-    else MPT_LAUNCH((k_ln_fwd<VPT, false, WARP, MAXT>), dim3((unsigned)grid), dim3((unsigned)threads), 0, st, p);
+    // one warp a row where that is possible; else the R in 2..4 that leaves the fewest of kLnWarps warps without work
+    // (8191 features: 11 warps of 3 vectors a lane rather than 8 of 4), the larger where two are alike
+    LnShape s = {c8 <= 32 ? 1 : (c8 <= 64 ? 2 : 4), 0, 0, 0};
+    if (c8 > 128) {
+        int best = 0;
+        for (int r = 4; r >= 2; r--) {
+            const int w = (c8 + 32 * r - 1) / (32 * r), busy = w <= kLnWarps ? kLnWarps / w * w : 0;
+            if (busy > best) { best = busy; s.R = r; }
+        }
+    }
+    s.row_warps = (c8 + 32 * s.R - 1) / (32 * s.R);
+    const int most = kLnWarps / s.row_warps, spread = (rows + 147) / 148;
+    s.groups = spread < most ? spread : most;
+    const long ctas = ((long)rows + s.groups - 1) / s.groups;
+    const long fit = 148L * per_sm * (kLnWarps / (s.groups * s.row_warps));
+    s.grid = (int)(ctas < fit ? ctas : fit);
+    return s;
+}
+
+template <typename P>
+cudaError_t ln_run(void (*kern)(const P), int id, const P &p, const LnShape &s, int inputs, cudaStream_t st)
+{
+    static bool configured[kMaxDevices][8] = {};
+    const int dev = current_device_slot();
+    if (dev < 0) return cudaErrorInvalidDevice;
+    const int warps = s.groups * s.row_warps;
+    const size_t smem = (size_t)warps * kLnBuffers * ((size_t)inputs * s.R * 32 * 16 + 8) + (inputs == 2 ? (size_t)s.row_warps * s.R * 512 : 0);
+    if (!configured[dev][id]) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   kLnWarps * kLnBuffers * (inputs * 4 * 32 * 16 + 8) + (inputs == 2 ? kLnWarps * 2048 : 0));
+        if (e != cudaSuccess) return e;
+        configured[dev][id] = true;
+    }
+    MPT_LAUNCH(kern, dim3((unsigned)s.grid), dim3((unsigned)(warps * 32)), smem, st, p);
     return cudaSuccess;
 }
 
-template <int VPT, bool WARP>
-cudaError_t run_bwd(const LnBwd &p, bool vec, int grid, int threads, cudaStream_t st)
-{
-    const size_t smem = WARP ? (size_t)8 * VPT * 256 * sizeof(float) : 0;
-    if (vec) MPT_LAUNCH((k_ln_bwd<VPT, true, WARP>), dim3((unsigned)grid), dim3((unsigned)threads), smem, st, p);
-    else MPT_LAUNCH((k_ln_bwd<VPT, false, WARP>), dim3((unsigned)grid), dim3((unsigned)threads), smem, st, p);
-    return cudaSuccess;
-}
-
-cudaError_t launch_ln_fwd(const LnFwd &p, cudaStream_t st)
+cudaError_t launch_ln_fwd(LnFwd p, cudaStream_t st)
 {
     const uintptr_t bits = (uintptr_t)p.x | (uintptr_t)p.y | (uintptr_t)p.gamma | (uintptr_t)p.beta;
     const bool vec = (bits & 15) == 0 && ((p.ldx | p.ldy) & 7) == 0;
     const int c8 = (p.cols + 7) / 8;
-    if (c8 <= 128) {
-        // a warp per row; few rows are spread over the SMs, one warp to a CTA
-        int warps = (p.rows + 147) / 148;
-        warps = warps < 1 ? 1 : (warps > 8 ? 8 : warps);
-        const long ctas = ((long)p.rows + warps - 1) / warps;
-        const int grid = (int)(ctas < 148 * 8 ? ctas : 148 * 8);
-        if (c8 <= 32) return run_fwd<1, true, 256>(p, vec, grid, warps * 32, st);
-        if (c8 <= 64) return run_fwd<2, true, 256>(p, vec, grid, warps * 32, st);
-        return run_fwd<4, true, 256>(p, vec, grid, warps * 32, st);
-    }
-    if (c8 <= 4 * 1024) {
-        const int threads = ((c8 + 3) / 4 + 31) / 32 * 32;
-        const int per_sm = threads <= 384 ? (1536 / threads < 16 ? 1536 / threads : 16) : 1;
-        const int grid = p.rows < 148 * per_sm ? p.rows : 148 * per_sm;
-        return threads <= 384 ? run_fwd<4, false, 384>(p, vec, grid, threads, st) : run_fwd<4, false, 1024>(p, vec, grid, threads, st);
+    if (c8 <= kLnMaxRowWarps * 128) {
+        const LnShape s = ln_shape(p.rows, c8, 2);
+        p.row_warps = s.row_warps;
+        if (s.R == 1) return vec ? ln_run(k_ln_fwd<1, true>, 0, p, s, 1, st) : ln_run(k_ln_fwd<1, false>, 1, p, s, 1, st);
+        if (s.R == 2) return vec ? ln_run(k_ln_fwd<2, true>, 2, p, s, 1, st) : ln_run(k_ln_fwd<2, false>, 3, p, s, 1, st);
+        if (s.R == 3) return vec ? ln_run(k_ln_fwd<3, true>, 4, p, s, 1, st) : ln_run(k_ln_fwd<3, false>, 5, p, s, 1, st);
+        return vec ? ln_run(k_ln_fwd<4, true>, 6, p, s, 1, st) : ln_run(k_ln_fwd<4, false>, 7, p, s, 1, st);
     }
     const int grid = p.rows < 296 ? p.rows : 296;
     if (vec) MPT_LAUNCH(k_ln_fwd_long<true>, dim3((unsigned)grid), dim3(1024), 0, st, p);
@@ -512,24 +769,21 @@ cudaError_t launch_ln_fwd(const LnFwd &p, cudaStream_t st)
     return cudaSuccess;
 }
 
-cudaError_t launch_ln_bwd(const LnBwd &p, uint16_t *dgamma, uint16_t *dbeta, uint32_t *nonfinite_flag, cudaStream_t st)
+cudaError_t launch_ln_bwd(LnBwd p, uint16_t *dgamma, uint16_t *dbeta, uint32_t *nonfinite_flag, cudaStream_t st)
 {
     const uintptr_t bits = (uintptr_t)p.x | (uintptr_t)p.dy | (uintptr_t)p.dx | (uintptr_t)p.gamma;
     const bool vec = (bits & 15) == 0 && ((p.ldx | p.lddy | p.lddx) & 7) == 0;
     const int c8 = (p.cols + 7) / 8;
     int nparts = 0;
     cudaError_t e = cudaSuccess;
-    if (p.rows > 0 && c8 <= 128) {
-        const int ctas = (p.rows + 7) / 8;
-        nparts = ctas < kLnMaxParts ? ctas : kLnMaxParts;
-        if (c8 <= 32) e = run_bwd<1, true>(p, vec, nparts, 256, st);
-        else if (c8 <= 64) e = run_bwd<2, true>(p, vec, nparts, 256, st);
-        else e = run_bwd<4, true>(p, vec, nparts, 256, st);
-    } else if (p.rows > 0 && c8 <= 2 * 768) {
-        const int threads = ((c8 + 1) / 2 + 31) / 32 * 32;
-        const int most = threads <= 384 ? 296 : 148;
-        nparts = p.rows < most ? p.rows : most;
-        e = run_bwd<2, false>(p, vec, nparts, threads, st);
+    if (p.rows > 0 && c8 <= kLnMaxRowWarps * 128) {
+        const LnShape s = ln_shape(p.rows, c8, 1);
+        p.row_warps = s.row_warps;
+        nparts = s.grid;
+        if (s.R == 1) e = vec ? ln_run(k_ln_bwd<1, true>, 0, p, s, 2, st) : ln_run(k_ln_bwd<1, false>, 1, p, s, 2, st);
+        else if (s.R == 2) e = vec ? ln_run(k_ln_bwd<2, true>, 2, p, s, 2, st) : ln_run(k_ln_bwd<2, false>, 3, p, s, 2, st);
+        else if (s.R == 3) e = vec ? ln_run(k_ln_bwd<3, true>, 4, p, s, 2, st) : ln_run(k_ln_bwd<3, false>, 5, p, s, 2, st);
+        else e = vec ? ln_run(k_ln_bwd<4, true>, 6, p, s, 2, st) : ln_run(k_ln_bwd<4, false>, 7, p, s, 2, st);
     } else if (p.rows > 0) {
         const int grid = p.rows < 296 ? p.rows : 296;
         if (vec) MPT_LAUNCH(k_ln_bwd_long<true>, dim3((unsigned)grid), dim3(1024), 0, st, p);
@@ -554,14 +808,14 @@ extern "C" {
 
 int mpt_layernorm_forward(int rows, int cols, const uint16_t *x_dev, int ldx, const uint16_t *gamma16_dev,
                           const uint16_t *beta16_dev, float eps, uint16_t *y_dev, int ldy, float *mean_dev, float *rstd_dev,
-                          void *cuda_stream)
+                          uint32_t *status_dev, void *cuda_stream)
 {
     if (!x_dev || !gamma16_dev || !y_dev || x_dev == y_dev) return MPT_ERR_INVALID_ARG;
     if (!(eps >= 0.0f) || !isfinite(eps)) return MPT_ERR_INVALID_ARG;
     if (rows < 0 || cols < 1 || cols > kLnMaxCols || ldx < cols || ldy < cols) return MPT_ERR_SHAPE;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (rows == 0) return MPT_OK;
-    const LnFwd p = {rows, cols, x_dev, (size_t)ldx, gamma16_dev, beta16_dev, eps, y_dev, (size_t)ldy, mean_dev, rstd_dev};
+    const LnFwd p = {rows, cols, 0, x_dev, (size_t)ldx, gamma16_dev, beta16_dev, eps, y_dev, (size_t)ldy, mean_dev, rstd_dev, status_dev};
     return launch_ln_fwd(p, st) == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
 }
 
@@ -575,8 +829,8 @@ int mpt_layernorm_workspace_bytes(int rows, int cols, size_t *bytes_out)
 
 int mpt_layernorm_backward(int rows, int cols, const uint16_t *dy_dev, int lddy, const uint16_t *x_dev, int ldx,
                            const uint16_t *gamma16_dev, const float *mean_dev, const float *rstd_dev, uint16_t *dx_dev, int lddx,
-                           uint16_t *dgamma16_dev, uint16_t *dbeta16_dev, uint32_t *nonfinite_flag_dev, void *workspace_dev,
-                           size_t workspace_bytes, void *cuda_stream)
+                           uint16_t *dgamma16_dev, uint16_t *dbeta16_dev, uint32_t *nonfinite_flag_dev, uint32_t *status_dev,
+                           void *workspace_dev, size_t workspace_bytes, void *cuda_stream)
 {
     if (!dy_dev || !x_dev || !gamma16_dev || !mean_dev || !rstd_dev || !dx_dev || !dgamma16_dev || !workspace_dev)
         return MPT_ERR_INVALID_ARG;
@@ -586,8 +840,8 @@ int mpt_layernorm_backward(int rows, int cols, const uint16_t *dy_dev, int lddy,
     mpt_layernorm_workspace_bytes(rows, cols, &need);
     if (workspace_bytes < need || ((uintptr_t)workspace_dev & 15) != 0) return MPT_ERR_WORKSPACE;
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    const LnBwd p = {rows, cols, dy_dev, (size_t)lddy, x_dev, (size_t)ldx, gamma16_dev, mean_dev, rstd_dev, dx_dev, (size_t)lddx,
-                     (float *)workspace_dev, ln_colp(cols)};
+    const LnBwd p = {rows, cols, 0, dy_dev, (size_t)lddy, x_dev, (size_t)ldx, gamma16_dev, mean_dev, rstd_dev, dx_dev, (size_t)lddx,
+                     (float *)workspace_dev, ln_colp(cols), status_dev};
     return launch_ln_bwd(p, dgamma16_dev, dbeta16_dev, nonfinite_flag_dev, st) == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
 }
 

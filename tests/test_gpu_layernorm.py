@@ -43,7 +43,7 @@ def forward(x, gamma, beta, eps, ld=None, shift=0, stats=True):
     from paper_1710_03740_b200 import binding as b
     rows, cols = x.shape
     ld = cols if ld is None else ld
-    xd, _ = pitched(x, ld, shift)
+    xd, _ = pitched(x, ld, shift, fill=float("nan"))       # what lies between the rows must not matter
     yd, ybuf = pitched(np.zeros_like(x), ld, shift, fill=7.0)
     yd.fill_(7.0)
     gd = torch.from_numpy(gamma).cuda()
@@ -62,8 +62,8 @@ def backward(dy, x, gamma, mean, rstd, ld=None, shift=0, want_beta=True, ws=None
     from paper_1710_03740_b200 import binding as b
     rows, cols = x.shape
     ld = cols if ld is None else ld
-    xd, _ = pitched(x, ld, shift)
-    dyd, _ = pitched(dy, ld, shift)
+    xd, _ = pitched(x, ld, shift, fill=float("nan"))
+    dyd, _ = pitched(dy, ld, shift, fill=float("nan"))
     dxd, dxbuf = pitched(np.zeros_like(x), ld, shift, fill=7.0)
     gd = torch.from_numpy(gamma).cuda()
     dg = torch.full((cols + 1,), 7.0, dtype=torch.float16, device="cuda")

@@ -15,14 +15,14 @@ def lib():
 
 
 def fwd(lib, **k):
-    a = dict(rows=4, cols=64, x=P(256), ldx=64, gamma=P(512), beta=P(768), eps=1e-5, y=P(1024), ldy=64, mean=None, rstd=None, st=None)
+    a = dict(rows=4, cols=64, x=P(256), ldx=64, gamma=P(512), beta=P(768), eps=1e-5, y=P(1024), ldy=64, mean=None, rstd=None, status=None, st=None)
     a.update(k)
     return lib.mpt_layernorm_forward(*a.values())
 
 
 def bwd(lib, **k):
     a = dict(rows=4, cols=64, dy=P(256), lddy=64, x=P(512), ldx=64, gamma=P(768), mean=P(1024), rstd=P(1280), dx=P(1536), lddx=64,
-             dgamma=P(1792), dbeta=P(2048), flag=None, ws=P(4096), nbytes=1 << 20, st=None)
+             dgamma=P(1792), dbeta=P(2048), flag=None, status=None, ws=P(4096), nbytes=1 << 20, st=None)
     a.update(k)
     return lib.mpt_layernorm_backward(*a.values())
 
