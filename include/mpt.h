@@ -563,7 +563,7 @@ int mpt_softmax_ce(const uint16_t *z_dev, int ldz, const int32_t *labels_dev, in
  * workspace: 256-byte aligned, mpt_linear_ce_workspace_bytes of the same N, V, H, row_block (want_dx, want_dW: whether
  * dx_dev, dW_dev will be given), owned by the caller and in use until the call's stream work has completed: calls
  * that may overlap, captured graphs among them, need one each.  The rows are worked on row_block at a time (a
- * multiple of 256; 0: the library's choice of 4096), which bounds the workspace: about 2 * row_block * V bytes of FP16
+ * multiple of 256, at most 65536; 0: the library's choice of 4096), which bounds the workspace: about 2 * row_block * V bytes of FP16
  * exponentials and 2 * row_block * H of x, and with more than one block 4 * V * H bytes in which dW is summed in FP32.
  * Results are run-to-run identical.  Asynchronous on the stream, which must belong to the current device. */
 #define MPT_LINEAR_CE_MAX_V (1 << 26)

@@ -546,18 +546,25 @@ def mpt_add_f16(a, lda, b, ldb, out, ldo, rows, cols, stream=None):
 
 # ------------------------------------------------------------ layer normalisation
 
+def _current_raw_stream(device):
+    """cudaStream_t of torch's current stream on a device.  torch's own accessor for the raw handle where it has it: building
+    a Stream object costs more than launching a small kernel."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw is not None else torch.cuda.current_stream(device).cuda_stream
+
+
 def _stream_of(stream, sizes):
     """Raw handle of `stream` (default: the current one) after a look at the tensors of a call: `sizes` lists
-    (tensor or None, bytes per element).  All have to be on the current device; pointers of another one
-    would reach the kernels unseen."""
+    (tensor or None, bytes per element).  All have to be on the stream's device; pointers of another one would reach
+    the kernels unseen."""
     import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    at = s.device_index
+    at = torch.cuda.current_device() if stream is None else stream.device_index
     for t, width in sizes:
-        if t is not None and (not t.is_cuda or t.get_device() != at or t.element_size() != width):
+        if t is not None and (t.get_device() != at or t.element_size() != width):
             raise ValueError("expected a CUDA tensor of %d-byte elements on the stream's device (cuda:%d), got %s on %s"
                              % (width, at, t.dtype, t.device))
-    return s.cuda_stream
+    return _current_raw_stream(at) if stream is None else stream.cuda_stream
 
 
 def _at(t):

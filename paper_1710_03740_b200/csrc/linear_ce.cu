@@ -27,6 +27,7 @@ namespace {
 constexpr int kGroup = 128;           // classes of one softmax group (CeEpi)
 constexpr float kLog2e = 1.4426950408889634f;      // as in the softmax epilogue
 constexpr int kDefaultRows = 4096;    // rows of a block when the caller does not choose
+constexpr int kMaxRows = 65536;       // largest block: CTAs of a pass over it stay inside 31 bits
 
 __device__ __forceinline__ float ex2(float x)
 {
@@ -107,15 +108,22 @@ __global__ void __launch_bounds__(256) k_ce_combine(const float2 *__restrict__ s
     }
 }
 
-// e -> 2^14 (p - [v = y]) in place.  A CTA takes 16384 neighbouring columns of one row (32 KB), 16 bytes a lane and
+// e -> 2^14 (p - [v = y]) in place, and the mean loss.  A CTA takes 16384 neighbouring columns of one row (32 KB), 16 bytes a lane and
 // load, all loads ahead of the first use.
 __global__ void __launch_bounds__(256) k_ce_rescale(uint16_t *__restrict__ e16, int ld, const float *__restrict__ factor, int groups,
                                                     int V, const int32_t *__restrict__ labels, const float *__restrict__ zlabel,
-                                                    const float2 *__restrict__ rowsum)
+                                                    const float2 *__restrict__ rowsum, const float *__restrict__ row_loss, int N,
+                                                    float *__restrict__ loss, int chunks)
 {
     pdl_trigger();
     pdl_wait();
-    const int row = blockIdx.y, col0 = blockIdx.x * 16384 + threadIdx.x * 8;
+    // one CTA more than there is work for, after the last block of rows: the mean loss
+    if (loss && blockIdx.x == gridDim.x - 1) {
+        __shared__ double red[256];
+        mean_of_rows(row_loss, N, loss, red);
+        return;
+    }
+    const int row = (int)(blockIdx.x / (unsigned)chunks), col0 = (int)(blockIdx.x % (unsigned)chunks) * 16384 + threadIdx.x * 8;
     uint16_t *er = e16 + (size_t)row * ld;
     const float *fr = factor + (size_t)row * groups;
     uint4 v[8];
@@ -273,7 +281,7 @@ extern "C" {
 int mpt_linear_ce_workspace_bytes(int N, int V, int H, int want_dx, int want_dW, int row_block, size_t *bytes_out)
 {
     if (!bytes_out) return MPT_ERR_INVALID_ARG;
-    if (N < 0 || V < 1 || V > MPT_LINEAR_CE_MAX_V || H < 8 || H % 8 || row_block < 0 || row_block % 256) return MPT_ERR_SHAPE;
+    if (N < 0 || V < 1 || V > MPT_LINEAR_CE_MAX_V || H < 8 || H % 8 || row_block < 0 || row_block > kMaxRows || row_block % 256) return MPT_ERR_SHAPE;
     *bytes_out = make_plan(N, V, H, want_dx != 0, want_dW != 0, row_block).total;
     return MPT_OK;
 }
@@ -285,7 +293,7 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
 {
     if (!x_dev || !W_dev || !labels_dev || !row_loss_dev || !loss_dev || !workspace_dev) return MPT_ERR_INVALID_ARG;
     if (!isfinite(S) || dx_dev == x_dev || dW_dev == W_dev) return MPT_ERR_INVALID_ARG;
-    if (N < 0 || V < 1 || V > MPT_LINEAR_CE_MAX_V || H < 8 || H % 8 || row_block < 0 || row_block % 256) return MPT_ERR_SHAPE;
+    if (N < 0 || V < 1 || V > MPT_LINEAR_CE_MAX_V || H < 8 || H % 8 || row_block < 0 || row_block > kMaxRows || row_block % 256) return MPT_ERR_SHAPE;
     if (ldx < H || ldw < H || (dx_dev && lddx < H) || (dW_dev && lddw < H)) return MPT_ERR_SHAPE;
     const uintptr_t bits = (uintptr_t)x_dev | (uintptr_t)W_dev | (uintptr_t)dx_dev | (uintptr_t)dW_dev;
     if ((bits & 15) || ldx % 8 || ldw % 8 || (dx_dev && lddx % 8) || (dW_dev && lddw % 8)) return MPT_ERR_SHAPE;
@@ -316,8 +324,11 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
         e = launch_pdl(k_ce_combine, dim3((unsigned)((R + 3) / 4)), dim3(256), 0, st, (const float2 *)stats, R, V, p.groups, labels,
                        (const float *)zlabel, rowsum, row_loss_dev + r0, bad_labels_dev, x, ldx, H, xs, factor);
         if (e != cudaSuccess || !grads) continue;
-        e = launch_pdl(k_ce_rescale, dim3((unsigned)((p.lde + 16383) / 16384), (unsigned)R), dim3(256), 0, st, e16, p.lde,
-                       (const float *)factor, p.groups, V, labels, (const float *)zlabel, (const float2 *)rowsum);
+        const bool last = b + 1 == p.blocks;
+        const int chunks = (p.lde + 16383) / 16384;
+        e = launch_pdl(k_ce_rescale, dim3((unsigned)chunks * (unsigned)R + (unsigned)last), dim3(256), 0, st, e16, p.lde,
+                       (const float *)factor, p.groups, V, labels, (const float *)zlabel, (const float2 *)rowsum,
+                       (const float *)row_loss_dev, N, last ? loss_dev : (float *)nullptr, chunks);
         if (e == cudaSuccess && dx_dev) {
             xd.alpha = alpha;
             xd.max_split = kDxSplit;
@@ -336,7 +347,7 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
                         status_dev, ws + p.splitk, p.splitk_bytes, st);
         }
     }
-    if (e == cudaSuccess) e = launch_loss_mean(row_loss_dev, N, loss_dev, st);
+    if (e == cudaSuccess && (!grads || N == 0)) e = launch_loss_mean(row_loss_dev, N, loss_dev, st);
     return e == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
 }
 

@@ -84,6 +84,20 @@ inline cudaError_t launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, siz
         if (launch_err_ != cudaSuccess) return launch_err_;  \
     } while (0)
 
+// *loss = mean of row_loss[0..B) by a CTA of 256 threads, in double and in a fixed order; red: 256 doubles.
+__device__ __forceinline__ void mean_of_rows(const float *row_loss, int B, float *loss, double *red)
+{
+    double acc = 0.0;
+    for (int i = threadIdx.x; i < B; i += 256) acc += (double)row_loss[i];
+    red[threadIdx.x] = acc;
+    __syncthreads();
+    for (int o = 128; o > 0; o >>= 1) {
+        if ((int)threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) *loss = (B > 0) ? (float)(red[0] / (double)B) : 0.0f;
+}
+
 __device__ __forceinline__ bool half_bits_nonfinite(uint32_t h) { return (h & 0x7C00u) == 0x7C00u; }
 __device__ __forceinline__ bool f32_nonfinite(float x)
 {

@@ -413,21 +413,13 @@ __global__ void __launch_bounds__(kSmaxThreads, 1) k_softmax_ce_bulk(const uint1
 
 
 
-// loss = (float)( sum_i (double)row_loss[i] / B ), fixed reduction order.
+// loss = (float)( sum_i (double)row_loss[i] / B ), fixed reduction order (mean_of_rows).
 __global__ void __launch_bounds__(256) k_loss_mean(const float *__restrict__ row_loss, int B, float *loss)
 {
     pdl_trigger();
     pdl_wait();
     __shared__ double red[256];
-    double acc = 0.0;
-    for (int i = threadIdx.x; i < B; i += 256) acc += (double)row_loss[i];
-    red[threadIdx.x] = acc;
-    __syncthreads();
-    for (int o = 128; o > 0; o >>= 1) {
-        if ((int)threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
-        __syncthreads();
-    }
-    if (threadIdx.x == 0) *loss = (B > 0) ? (float)(red[0] / (double)B) : 0.0f;
+    mean_of_rows(row_loss, B, loss, red);
 }
 
 cudaError_t launch_loss_mean(const float *row_loss, int B, float *loss, cudaStream_t st)
