@@ -566,7 +566,7 @@ int mpt_softmax_ce(const uint16_t *z_dev, int ldz, const int32_t *labels_dev, in
  * multiple of 256, at most 65536; 0: the library's choice of 4096), which bounds the workspace: about 2 * row_block * V bytes of FP16
  * exponentials and 2 * row_block * H of x, and with more than one block 4 * V * H bytes in which dW is summed in FP32.
  * Results are run-to-run identical.  Asynchronous on the stream, which must belong to the current device. */
-#define MPT_LINEAR_CE_MAX_V (1 << 26)
+#define MPT_LINEAR_CE_MAX_V (1 << 24)
 int mpt_linear_ce_workspace_bytes(int N, int V, int H, int want_dx, int want_dW, int row_block, size_t *bytes_out);
 int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uint16_t *W_dev, int ldw, const int32_t *labels_dev,
                   float S, int row_block, uint16_t *dx_dev, int lddx, uint16_t *dW_dev, int lddw, float *row_loss_dev,

@@ -494,7 +494,7 @@ static cudaError_t launch_bn(int op, int M, int N, int K, const uint16_t *A, int
 // graph on 2048x1024x8192, 1024x1024x4096, 512x256x4096 and the tiny-MLP products.  The split
 // is only considered when a workspace is available.
 void tc_gemm_plan(int M, int N, int K, size_t ws_bytes, int *bn_out, int *split_out, size_t *ws_needed, double *cost_out,
-                  int max_split)
+                  int max_split, int min_split)
 {
     const long tm = (M + BLOCK_M - 1) / BLOCK_M;
     const int nkb = (K + BLOCK_K - 1) / BLOCK_K;
@@ -504,8 +504,8 @@ void tc_gemm_plan(int M, int N, int K, size_t ws_bytes, int *bn_out, int *split_
         if (bn < 256 && N <= bn) continue;
         const long tiles = tm * ((N + bn - 1) / bn);
         const double cyc = bn == 256 ? 600.0 : (bn == 128 ? 437.0 : 450.0);
-        for (int s = 1; s <= max_split; s++) {
-            if (s > 1 && (nkb / s < 8)) break;
+        for (int s = min_split; s <= max_split; s++) {
+            if (s > min_split && (nkb / s < 8)) break;
             const size_t need = s > 1 ? (size_t)s * M * (((size_t)N + 31) / 32 * 32) * 4 : 0;
             if (need > ws_bytes) break;
             const long rounds = (tiles * s + 147) / 148;
@@ -567,7 +567,7 @@ cudaError_t launch_gemm_tc(int op, int M, int N, int K, const uint16_t *A, int l
     p.nonfinite_flag = nonfinite_flag;
     p.status = status;
     int bn = 256, split = 1;
-    tc_gemm_plan(M, N, K, (splitk_ws && (((uintptr_t)splitk_ws) & 15) == 0) ? splitk_ws_bytes : 0, &bn, &split, nullptr, nullptr, x.max_split);
+    tc_gemm_plan(M, N, K, (splitk_ws && (((uintptr_t)splitk_ws) & 15) == 0) ? splitk_ws_bytes : 0, &bn, &split, nullptr, nullptr, x.max_split, x.min_split);
     if (x.ce && bn < 128) bn = 128;
     p.split_k = split;
     p.partial = splitk_ws;

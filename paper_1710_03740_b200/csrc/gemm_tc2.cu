@@ -69,7 +69,9 @@ struct Params {
     // a unit leaves its raw FP32 accumulator in partial[part][M][ldp] and a second kernel adds the
     // parts in ascending order and applies the epilogue.  split_k == 1: off.
     int split_k;
-    int split_major;                 // units of one part are neighbours (they share its operands), not the parts of one tile
+    // > 0: that many pairs side by side on a tile; all tiles' first parts come first, then their second ones (the tiles of
+    // a part are neighbours and share its operand panels; split_k / split_side parts of a tile follow one another on one pair)
+    int split_side;
     float *partial;
     int ldp;
     // tail split: the tiles left over for a last, partly filled round are cut into tail_split units
@@ -119,8 +121,14 @@ __device__ __forceinline__ Unit unit_of(const Params &p, int u, int nkb)
     w.tail_slot = -1;
     if (p.split_k > 1) {            // parts of one tile are neighbouring units: they run side by side
         const int tiles = p.tiles_m * p.tiles_n;
-        tile = p.split_major ? u % tiles : u / p.split_k;
-        w.part = p.split_major ? u / tiles : u - tile * p.split_k;
+        if (p.split_side > 0) {
+            const int q = u / tiles, side = q % p.split_side, seq = q / p.split_side;
+            tile = u - q * tiles;
+            w.part = side * (p.split_k / p.split_side) + seq;
+        } else {
+            tile = u / p.split_k;
+            w.part = u - tile * p.split_k;
+        }
         w.kb0 = (int)(((long long)nkb * w.part) / p.split_k);
         w.kb1 = (int)(((long long)nkb * (w.part + 1)) / p.split_k);
     } else if (u >= p.full_units && p.tail_split > 1) {
@@ -558,7 +566,8 @@ static cudaError_t launch_variant(const CUtensorMap &ta, const CUtensorMap &tb, 
         p.full_units = tiles;
         p.num_units = tiles;
     }
-    const int grid_pairs = p.num_units < max_pairs ? p.num_units : max_pairs;
+    int grid_pairs = p.num_units < max_pairs ? p.num_units : max_pairs;
+    if (p.split_side > 0 && tiles * p.split_side <= max_pairs) grid_pairs = tiles * p.split_side;      // in step to the end
     cfg.gridDim = dim3(2 * grid_pairs, 1, 1);
     cfg.numAttrs = 2;
     cudaError_t e = cudaLaunchKernelEx(&cfg, kern, ta, tb, tbh, tc, p);
@@ -691,14 +700,14 @@ cudaError_t launch_gemm_tc2(int op, int M, int N, int K, const uint16_t *A, int 
     }
     p.full_units = p.num_units = 0;
     p.split_k = 1;
-    p.split_major = x.split > 0 ? 1 : 0;
+    p.split_side = x.split;
     p.partial = nullptr;
     p.ldp = (N + 31) / 32 * 32;
     p.tail_split = 1;
     p.tail_partial = nullptr;
     if (!lstm && splitk_ws && (((uintptr_t)splitk_ws) & 15) == 0) {
         int split = 1;
-        if (x.split > 0) split = x.split;      // the caller has sized the scratch for it
+        if (x.split > 0) split = x.split * x.split_seq;      // the caller has sized the scratch for it
         else tc2_split_plan(M, N, K, splitk_ws_bytes, &split, nullptr, nullptr);
         if (split > 1) {
             p.split_k = split;

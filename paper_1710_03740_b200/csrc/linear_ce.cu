@@ -171,7 +171,7 @@ struct Plan {
     int lde;              // pitch of the exponentials
     int groups;
     int ldacc;
-    size_t e16, stats, factor, rowsum, zlabel, xs, splitk, splitk_bytes, acc32, total;
+    size_t e16, stats, factor, rowsum, zlabel, xs, splitk, splitk_bytes, dx32, acc32, total;
 };
 
 // The split of dx's contraction over the vocabulary: for few rows the product has few tiles and reading W is what
@@ -184,6 +184,13 @@ constexpr int kDxSplit = 64;
 // once from DRAM; in 9 parts, two rounds and 97 % of the pairs busy, the second round's units start apart and nothing is
 // shared any more (7.8 instead of 3.4 GB read, 1.53 ms); two pairs per tile in one cluster leave 57 % of the SMs idle
 // (1.82 ms).  A part keeps at least 64 k-blocks, under which the FP32 parts' way through L2 disappears.
+// Whatever the kernel, no accumulator sums more than kDxPart terms: the tensor core's FP32 sums lose up to half a step
+// at each of their K / 16 additions, always towards zero, which over 793471 terms is 4e-4 of the sum - more than all
+// FP16 roundings together.  The parts are added with correct rounding.
+constexpr int kDxPart = 32768;
+
+int dx_parts(int V) { return (V + kDxPart - 1) / kDxPart; }
+
 int dx_pair_split(int M, int N, int K)
 {
     if (M < 256 || N < 256) return 0;
@@ -193,16 +200,24 @@ int dx_pair_split(int M, int N, int K)
     while (s > 1 && nkb / s < 64) s--;
     return s > 1 ? s : 0;
 }
+// Parts that one pair works off one after the other beside s - 1 others.
+int dx_pair_seq(int s, int K) { return (dx_parts(K) + s - 1) / s; }
+// dx on the CTA-pair kernel with more tiles than that: one launch per part of the contraction, FP32 sums in between.
+bool dx_in_launches(int M, int N, int K) { return dx_parts(K) > 1 && !dx_pair_split(M, N, K) && tc2_gemm_preferred(M, N, K); }
 
-size_t product_scratch(int op, int M, int N, int K, int max_split)
+// Scratch of dx's and dW's products besides the FP32 sums.
+size_t product_scratch(int op, int M, int N, int K)
 {
-    if (op == MPT_OP_DGRAD)
-        if (const int s = dx_pair_split(M, N, K)) return (size_t)s * M * ((N + 31) / 32 * 32) * sizeof(float);
+    if (op == MPT_OP_DGRAD) {
+        if (const int s = dx_pair_split(M, N, K)) return (size_t)s * dx_pair_seq(s, K) * M * ((N + 31) / 32 * 32) * sizeof(float);
+        if (dx_in_launches(M, N, K)) return 0;
+    }
     if (tc4_split_for(M, N, K)) return 0;
     size_t need = 0;
     if (tc2_gemm_preferred(M, N, K)) return tc2_tail_ws_bytes(M, N, K);
+    const int least = op == MPT_OP_DGRAD ? dx_parts(K) : 1, most = op == MPT_OP_DGRAD ? (least > kDxSplit ? least : kDxSplit) : 8;
     int bn, split;
-    tc_gemm_plan(M, N, K, (size_t)1 << 40, &bn, &split, &need, nullptr, max_split);
+    tc_gemm_plan(M, N, K, (size_t)1 << 40, &bn, &split, &need, nullptr, most, least);
     return need;
 }
 
@@ -224,21 +239,24 @@ Plan make_plan(int N, int V, int H, bool want_dx, bool want_dW, int row_block)
     p.rowsum = take((size_t)p.R * sizeof(float2));
     p.zlabel = take((size_t)p.R * sizeof(float));
     p.xs = take(want_dW ? (size_t)p.R * H * 2 : 0);
-    size_t sk = 0;
+    size_t sk = 0, acc = 0;
     if (want_dx) {
-        sk = product_scratch(MPT_OP_DGRAD, p.R, H, V, kDxSplit);
+        sk = product_scratch(MPT_OP_DGRAD, p.R, H, V);
+        if (dx_in_launches(p.R, H, V)) acc = (size_t)p.R * p.ldacc * sizeof(float);
         const int rest = N - (p.blocks - 1) * p.R;          // the last block may be shorter
         if (p.blocks > 1 && rest != p.R) {
-            const size_t s2 = product_scratch(MPT_OP_DGRAD, rest, H, V, kDxSplit);
+            const size_t s2 = product_scratch(MPT_OP_DGRAD, rest, H, V);
             sk = s2 > sk ? s2 : sk;
+            if (dx_in_launches(rest, H, V) && acc == 0) acc = (size_t)rest * p.ldacc * sizeof(float);
         }
     }
     if (want_dW && p.blocks == 1) {
-        const size_t s2 = product_scratch(MPT_OP_WGRAD, V, H, p.R, 8);
+        const size_t s2 = product_scratch(MPT_OP_WGRAD, V, H, p.R);
         sk = s2 > sk ? s2 : sk;
     }
     p.splitk_bytes = sk;
     p.splitk = take(sk);
+    p.dx32 = take(acc);
     p.acc32 = take(want_dW && p.blocks > 1 ? (size_t)V * p.ldacc * sizeof(float) : 0);
     p.total = at;
     return p;
@@ -259,6 +277,7 @@ cudaError_t product(int op, int M, int N, int K, const uint16_t *A, int lda, con
         if (const int s = dx_pair_split(M, N, K)) {
             ProductExtra y = x;
             y.split = s;
+            y.split_seq = dx_pair_seq(s, K);
             return launch_gemm_tc2(op, M, N, K, A, lda, B, ldb, C, ldc, false, nullptr, 0, nonfinite, status, st, nullptr, ws, ws_bytes, &y);
         }
     }
@@ -331,9 +350,24 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
                        (const float *)row_loss_dev, N, last ? loss_dev : (float *)nullptr, chunks);
         if (e == cudaSuccess && dx_dev) {
             xd.alpha = alpha;
-            xd.max_split = kDxSplit;
-            e = product(MPT_OP_DGRAD, R, H, V, e16, p.lde, W_dev, ldw, dx_dev + (size_t)r0 * lddx, lddx, xd, nullptr, status_dev,
-                        ws + p.splitk, p.splitk_bytes, st);
+            uint16_t *dx = dx_dev + (size_t)r0 * lddx;
+            const int parts = dx_parts(V);
+            if (dx_in_launches(R, H, V)) {
+                xd.acc32 = (float *)(ws + p.dx32);
+                xd.ldacc = p.ldacc;
+                const int step = ((V + parts - 1) / parts + 7) / 8 * 8;        // operands stay 16-byte aligned
+                for (int v = 0; v < V && e == cudaSuccess; v += step) {
+                    xd.acc_add = v > 0;
+                    xd.acc_store = v + step < V;
+                    e = launch_gemm_tc2(MPT_OP_DGRAD, R, H, V - v < step ? V - v : step, e16 + v, p.lde, W_dev + (size_t)v * ldw, ldw, dx,
+                                        lddx, false, nullptr, 0, nullptr, status_dev, st, nullptr, nullptr, 0, &xd);
+                }
+            } else {
+                xd.min_split = parts;
+                xd.max_split = parts > kDxSplit ? parts : kDxSplit;
+                e = product(MPT_OP_DGRAD, R, H, V, e16, p.lde, W_dev, ldw, dx, lddx, xd, nullptr, status_dev, ws + p.splitk,
+                            p.splitk_bytes, st);
+            }
         }
         if (e == cudaSuccess && dW_dev) {
             xw.alpha = alpha;

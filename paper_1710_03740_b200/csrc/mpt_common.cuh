@@ -140,7 +140,10 @@ struct ProductExtra {
     int acc_add = 0, acc_store = 0;
     const CeEpi *ce = nullptr;    // softmax epilogue (forward products)
     int max_split = 8;            // single-CTA kernel: most parts the contraction may be cut into
-    int split = 0;                // CTA-pair kernel: cut the contraction into this many parts, part by part (0: its own choice)
+    int min_split = 1;            // ... and the fewest
+    // CTA-pair kernel (0: its own choice): cut the contraction into split * split_seq parts; `split` CTA pairs work side by
+    // side on a tile, each on split_seq parts one after the other
+    int split = 0, split_seq = 1;
 };
 
 // Launchers (each returns a cudaError_t from the launch; all asynchronous on `st`).
@@ -227,7 +230,7 @@ cudaError_t launch_gemm_tc(int op, int M, int N, int K, const uint16_t *A, int l
                            uint32_t *nonfinite_flag, uint32_t *status, cudaStream_t st, float *splitk_ws = nullptr,
                            size_t splitk_ws_bytes = 0, const LstmEpi *lstm = nullptr, const ProductExtra *extra = nullptr);
 void tc_gemm_plan(int M, int N, int K, size_t ws_bytes, int *bn_out, int *split_out, size_t *ws_needed,
-                  double *cost_out = nullptr, int max_split = 8);
+                  double *cost_out = nullptr, int max_split = 8, int min_split = 1);
 // Kernel choice for a product the tensor-core path takes: true = CTA-pair kernel (possibly with a
 // split contraction), false = single-CTA kernel; ws_needed = scratch the choice would like.
 bool tc_choose_pair(int M, int N, int K, size_t ws_bytes, size_t *ws_needed);

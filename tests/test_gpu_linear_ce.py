@@ -103,7 +103,8 @@ def check(x, W, y, S, got):
 
 
 SIZES = [(1, 1, 8), (1, 2, 8), (3, 7, 16), (5, 128, 24), (64, 1000, 512), (63, 1001, 520), (128, 129, 64), (129, 257, 72),
-         (300, 5003, 256), (700, 20000, 136), (257, 19001, 64), (2, 100003, 64), (130, 40000, 40), (1000, 3001, 1000)]
+         (300, 5003, 256), (700, 20000, 136), (257, 19001, 64), (2, 100003, 64), (130, 40000, 40), (1000, 3001, 1000),
+         (300, 70001, 264), (1024, 200003, 1024), (2048, 70001, 2560), (2050, 33000, 1280)]
 
 
 @pytest.mark.parametrize("N,V,H", SIZES)
