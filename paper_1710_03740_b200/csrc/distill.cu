@@ -347,6 +347,8 @@ __device__ __forceinline__ void bulk_out(void *dst, uint32_t src, uint32_t bytes
 // Shared memory: buffers [nw][ns][per] of 16-byte vectors | entries [nb] | mbarriers: [nw][ns] of the buffers, [4] of
 // the pairs, 2 x [nb] of the entries (full, empty) | pairs [4][cl * nw] | hash tables [teachers] | the row's pair [nb] |
 // live [nb] | abort word
+// mbarriers of the buffers: one per warp and buffer, or two per buffer where a warp of its own moves whole rows
+__host__ __device__ inline int buffer_bars(int nw, int ns) { return (nw < 2 ? 2 : nw) * ns; }
 struct Layout {
     uint32_t ent, bars, red, table, pair, live, abort, total;
     int slots;
@@ -359,7 +361,7 @@ __host__ __device__ inline Layout layout_of(int nw, int ns, int per, int cl, int
     at += (uint32_t)nb * ((uint32_t)K * kEntryWords + kMaxWarps + 1u) * 4u;
     at = (at + 7u) & ~7u;
     l.bars = at;
-    at += ((uint32_t)nw * (uint32_t)ns + (uint32_t)kPairBuffers + 2u * (uint32_t)nb) * 8u;
+    at += ((uint32_t)buffer_bars(nw, ns) + (uint32_t)kPairBuffers + 2u * (uint32_t)nb) * 8u;
     l.red = at;
     at += (uint32_t)kPairBuffers * (uint32_t)cl * (uint32_t)nw * 8u;
     l.slots = 32;
@@ -395,8 +397,10 @@ static __device__ __noinline__ bool wait_asleep(uint32_t bar, uint32_t parity, v
 }
 
 // What all warps of a CTA share, and each warp's part of the rows.  BULK: rows start on 16-byte boundaries and move by
-// bulk copies (a last, partial vector by element accesses); otherwise the warp copies elements.
-template <bool BULK>
+// bulk copies; otherwise the warps copy elements.  ROWS: the CTA's part of a row lies in one buffer of [ns] and moves as one
+// copy, in and out, by a warp that does nothing else: what a warp spends on issuing its own copies it spends once a row, and
+// all others wait for the slowest.  Otherwise each warp has ns buffers of its own.
+template <bool BULK, bool ROWS>
 struct Cta {
     const DistillArgs &p;
     uint8_t *smem;
@@ -408,6 +412,7 @@ struct Cta {
     // this warp's part: vectors [v0, v0 + nv) of a row, its buffers and their mbarriers
     int v0, nv;
     uint4 *buf;
+    int pitch;           // vectors from one buffer to the next
     uint32_t bar0;
 
     __device__ __forceinline__ Cta(const DistillArgs &args, uint8_t *s) : p(args), smem(s), L(layout_of(args.nw, args.ns, args.per, args.cl, args.K, 1 << args.nb_log2))
@@ -425,10 +430,16 @@ struct Cta {
         v0 = rank * p.vp + warp * p.wv;
         nv = warp < p.nw ? max(0, min(v_end, v0 + p.wv) - v0) : 0;
         if (nv == 0) v0 = 0;
-        buf = (uint4 *)smem + (size_t)warp * p.ns * p.per;
-        bar0 = bars + 8u * (uint32_t)(warp * p.ns);
-        if (warp < p.nw && lane == 0)
+        buf = (uint4 *)smem + (ROWS ? (size_t)warp * p.wv : (size_t)warp * p.ns * p.per);
+        pitch = ROWS ? p.nw * p.wv : p.per;
+        bar0 = ROWS ? bars : bars + 8u * (uint32_t)(warp * p.ns);
+        if (!ROWS && warp < p.nw && lane == 0)
             for (int i = 0; i < p.ns; i++) mbar_init(bar0 + 8u * (uint32_t)i, 1);
+        if (ROWS && threadIdx.x == 0)
+            for (int i = 0; i < p.ns; i++) {
+                mbar_init(bar0 + 8u * (uint32_t)i, 1);                        // the row has arrived
+                mbar_init(written_bar(i), (uint32_t)p.nw);                    // every warp has put its gradient in its place
+            }
         if (threadIdx.x == 0) {
             for (int i = 0; i < kPairBuffers; i++) mbar_init(pair_bar(i), (uint32_t)pairs);
             for (int b = 0; b < 1 << p.nb_log2; b++) {
@@ -442,9 +453,10 @@ struct Cta {
         __syncthreads();
         if (p.cl > 1) cluster_sync_all();   // every CTA of the cluster has its barriers before anything arrives there
     }
-    __device__ __forceinline__ uint32_t pair_bar(int i) const { return bars + 8u * (uint32_t)(p.nw * p.ns + (i & (kPairBuffers - 1))); }
-    __device__ __forceinline__ uint32_t full_bar(int b) const { return bars + 8u * (uint32_t)(p.nw * p.ns + kPairBuffers + b); }
+    __device__ __forceinline__ uint32_t pair_bar(int i) const { return bars + 8u * (uint32_t)(buffer_bars(p.nw, p.ns) + (i & (kPairBuffers - 1))); }
+    __device__ __forceinline__ uint32_t full_bar(int b) const { return bars + 8u * (uint32_t)(buffer_bars(p.nw, p.ns) + kPairBuffers + b); }
     __device__ __forceinline__ uint32_t empty_bar(int b) const { return full_bar(b) + (8u << p.nb_log2); }
+    __device__ __forceinline__ uint32_t written_bar(int s) const { return bars + 8u * (uint32_t)(p.ns + s); }
     __device__ __forceinline__ Entries entries(int b) const
     {
         float *at = (float *)(smem + L.ent) + b * (kEntryWords * p.K + kMaxWarps + 1);
@@ -478,7 +490,7 @@ struct Cta {
     {
         if (BULK && (v0 + f + n) * 8 > p.C) {
             if (copied(i, f, n) == n && lane < 8 && (v0 + f + n - 1) * 8 + lane >= p.C)
-                ((uint16_t *)(buf + s * p.per + n - 1))[lane] = (uint16_t)kNegInf16;
+                ((uint16_t *)(buf + s * pitch + n - 1))[lane] = (uint16_t)kNegInf16;
             __syncwarp();
         }
     }
@@ -486,7 +498,7 @@ struct Cta {
     __device__ __forceinline__ void request(int i, int s, int f, int n, uint64_t policy)
     {
         const uint16_t *src = p.z + (size_t)row_of(i) * p.ldz + (size_t)(v0 + f) * 8;
-        uint4 *dst = buf + s * p.per;
+        uint4 *dst = buf + s * pitch;
         if (BULK) {
             const int whole = copied(i, f, n);
             if (lane == 0) {                                          // each use of a buffer completes one phase of its barrier
@@ -507,29 +519,70 @@ struct Cta {
     {
         if (BULK) wait<false>(bar0 + 8u * (uint32_t)s, parity);
     }
-    // Writes this warp's gradient of row i from buffer s; commits one bulk group.
-    __device__ __forceinline__ void send(int i, int s, uint64_t policy)
+    // ROWS: the work of the last warp.  Every buffer goes round: a row arrives, its gradient takes its place, leaves, and the
+    // row ns further arrives.
+    __device__ __forceinline__ void move_rows()
+    {
+        const uint64_t policy = l2_policy(2);        // every byte is used once
+        const int first = rank * p.vp, n = max(0, min((p.C + 7) / 8, first + p.vp) - first);
+        auto bring = [&](int i, int s) {
+            const uint16_t *src = p.z + (size_t)row_of(i) * p.ldz + (size_t)first * 8;
+            uint4 *dst = (uint4 *)smem + s * pitch;
+            // a partial vector at the row's end as in copied()
+            const int whole = row_of(i) == p.B - 1 ? min(n, p.C / 8 - first) : n;
+            if (whole < n && lane < 8) {
+                const int e = (first + whole) * 8 + lane;
+                ((uint16_t *)(dst + whole))[lane] = e < p.C ? src[whole * 8 + lane] : (uint16_t)kNegInf16;
+            }
+            __syncwarp();                            // the arrival below tells of these, too
+            if (lane == 0) {
+                if (whole > 0) bulk_in(smem_u32(dst), src, (uint32_t)whole * 16u, bar0 + 8u * (uint32_t)s, policy);
+                else mbar_arrive(bar0 + 8u * (uint32_t)s);
+            }
+        };
+        for (int i = 0; i < p.ns && i < n_rows; i++) bring(i, i);
+        int s = 0;
+        uint32_t parity = 0;
+        for (int i = 0; i < n_rows; i++) {
+            wait<false>(written_bar(s), parity);
+            if (p.dz && lane == 0) {
+                const int whole = min(n, p.C / 8 - first);      // the owner of a partial vector stores its elements itself
+                if (whole > 0 && !dead)
+                    bulk_out(p.dz + (size_t)row_of(i) * p.lddz + (size_t)first * 8, smem_u32((uint4 *)smem + s * pitch), (uint32_t)whole * 16u, policy);
+                bulk_commit_group();
+                bulk_wait_group_read<0>();
+            }
+            __syncwarp();
+            if (i + p.ns < n_rows) bring(i + p.ns, s);
+            if (++s == p.ns) {
+                s = 0;
+                parity ^= 1u;
+            }
+        }
+    }
+    // ROWS: this warp's gradient of row i is in its place in buffer s.
+    __device__ __forceinline__ void written(int i, int s)
+    {
+        if (p.dz) {
+            const int whole = min(nv, p.C / 8 - v0);
+            if (nv > 0 && whole < nv && lane < 8 && !dead) {
+                const int e = (v0 + whole) * 8 + lane;
+                if (e < p.C) out(i)[whole * 8 + lane] = ((const uint16_t *)(buf + s * pitch + whole))[lane];
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(written_bar(s));
+    }
+    // Writes this warp's gradient of row i from buffer s, element by element.
+    __device__ __forceinline__ void send(int i, int s)
     {
         uint16_t *dst = out(i);
-        const uint4 *src = buf + s * p.per;
-        if (BULK) {
-            const int whole = min(nv, p.C / 8 - v0);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) {
-                if (whole > 0 && !dead) bulk_out(dst, smem_u32(src), (uint32_t)whole * 16u, policy);
-                bulk_commit_group();
-            }
-            if (whole < nv && lane < 8 && !dead) {
-                const int e = (v0 + whole) * 8 + lane;
-                if (e < p.C) dst[whole * 8 + lane] = ((const uint16_t *)(src + whole))[lane];
-            }
-        } else {
-            __syncwarp();
-            if (!dead)
-                for (int e = lane; e < nv * 8; e += 32)
-                    if (v0 * 8 + e < p.C) dst[e] = ((const uint16_t *)src)[e];
-        }
+        const uint4 *src = buf + s * pitch;
+        __syncwarp();
+        if (!dead)
+            for (int e = lane; e < nv * 8; e += 32)
+                if (v0 * 8 + e < p.C) dst[e] = ((const uint16_t *)src)[e];
         __syncwarp();
     }
     // Where this warp's gradient of row i goes.
@@ -630,31 +683,30 @@ struct Cta {
 
 // Rows whose exponentials stay in registers: R vectors per lane.
 template <int R, bool BULK>
-__global__ void __launch_bounds__((kMaxWarps + kTeachers) * 32, 1) k_distill(const DistillArgs p)
+__global__ void __launch_bounds__((kMaxWarps + kTeachers + 1) * 32, 1) k_distill(const DistillArgs p)
 {
     pdl_trigger();
     pdl_wait();
     extern __shared__ __align__(128) uint8_t smem[];
-    Cta<BULK> c(p, smem);
+    Cta<BULK, BULK> c(p, smem);
     if (c.warp >= p.nw) {
-        c.teach();
+        if (c.warp < p.nw + kTeachers) c.teach();
+        else if (BULK) c.move_rows();
         c.leave();
         return;
     }
-    const uint64_t policy = l2_policy(2);        // every byte is used once
     const int nv = c.nv;
     int s_ask = 0, s_use = 0;
     uint32_t parity = 0;
     auto ask = [&](int i) {
-        if (nv > 0 && i < c.n_rows) {
-            c.request(i, s_ask, 0, nv, policy);
+        if (!BULK && nv > 0 && i < c.n_rows) {
+            c.request(i, s_ask, 0, nv, 0);
             s_ask = s_ask + 1 == p.ns ? 0 : s_ask + 1;
         }
     };
     for (int i = 0; i + 1 < p.ns; i++) ask(i);
     for (int i = 0; i < c.n_rows; i++) {
-        // the buffer that row i + ns - 1 goes into held row i - 1, whose gradient has had most of this iteration to leave it
-        uint4 *v = c.buf + s_use * p.per;
+        uint4 *v = c.buf + s_use * c.pitch;
         float e[R][8];
         float m = -INFINITY, b = 0.0f, s = 0.0f;
         if (nv > 0) {
@@ -708,12 +760,9 @@ __global__ void __launch_bounds__((kMaxWarps + kTeachers) * 32, 1) k_distill(con
                 for (int j = c.lane; j < nv; j += 32) v[j] = make_uint4(0u, 0u, 0u, 0u);
             }
         }
-        if (nv > 0 && i + p.ns - 1 < c.n_rows) {
-            if (c.lane == 0) bulk_wait_group_read<0>();
-            __syncwarp();
-            ask(i + p.ns - 1);
-        }
-        if (p.dz && nv > 0) c.send(i, s_use, policy);
+        if (BULK) c.written(i, s_use);
+        else if (p.dz && nv > 0) c.send(i, s_use);
+        ask(i + p.ns - 1);
         c.close_entries(eb, pr);
         if (++s_use == p.ns) {
             s_use = 0;
@@ -731,7 +780,7 @@ __global__ void __launch_bounds__((kMaxWarps + kTeachers) * 32, 1) k_distill_str
     pdl_trigger();
     pdl_wait();
     extern __shared__ __align__(128) uint8_t smem[];
-    Cta<BULK> c(p, smem);
+    Cta<BULK, false> c(p, smem);
     if (c.warp >= p.nw) {
         c.teach();
         c.leave();
@@ -809,8 +858,9 @@ constexpr uint32_t kSmemLimit = 220u * 1024u;
 
 typedef void (*DistillKernel)(const DistillArgs);
 
-// id: a number of its own for each kernel (what is known about it is kept per device)
-cudaError_t run(DistillKernel kern, int id, const DistillArgs &p, uint32_t smem, cudaStream_t st)
+// id: a number of its own for each kernel (what is known about it is kept per device); extra: warps besides those that
+// hold logits and the teacher's
+cudaError_t run(DistillKernel kern, int id, int extra, const DistillArgs &p, uint32_t smem, cudaStream_t st)
 {
     static bool configured[kMaxDevices][32] = {};
     static int resident[kMaxDevices][9] = {};       // clusters of a size that the device holds, one CTA per SM; 0 = not asked yet
@@ -835,7 +885,7 @@ cudaError_t run(DistillKernel kern, int id, const DistillArgs &p, uint32_t smem,
     // clusters than are resident at once.
     if (resident[dev][p.cl] == 0) {
         cfg.gridDim = dim3((unsigned)(148 / p.cl * p.cl));
-        cfg.blockDim = dim3((kMaxWarps + kTeachers) * 32);
+        cfg.blockDim = dim3((kMaxWarps + kTeachers + extra) * 32);
         cfg.dynamicSmemBytes = kSmemLimit;
         cfg.numAttrs = 1;
         int n = 0;
@@ -844,8 +894,8 @@ cudaError_t run(DistillKernel kern, int id, const DistillArgs &p, uint32_t smem,
         if (n < 1) return cudaErrorLaunchOutOfResources;
         resident[dev][p.cl] = n;
     }
-    const int threads = (p.nw + kTeachers) * 32;
-    int per_sm = (kMaxWarps + kTeachers) * 32 / threads;          // what the kernel's registers allow
+    const int threads = (p.nw + kTeachers + extra) * 32;
+    int per_sm = (kMaxWarps + kTeachers + extra) * 32 / threads;          // what the kernel's registers allow
     const int by_smem = (int)((227u * 1024u) / (smem + 1024u));
     if (by_smem < per_sm) per_sm = by_smem;
     if (per_sm < 1) per_sm = 1;
@@ -863,7 +913,7 @@ cudaError_t launch_rounds(int rounds, const DistillArgs &p, uint32_t smem, cudaS
 {
     static const DistillKernel kern[kMaxRounds] = {k_distill<1, BULK>, k_distill<2, BULK>, k_distill<3, BULK>, k_distill<4, BULK>,
                                                    k_distill<5, BULK>, k_distill<6, BULK>, k_distill<7, BULK>, k_distill<8, BULK>};
-    return run(kern[rounds - 1], (BULK ? 0 : kMaxRounds) + rounds - 1, p, smem, st);
+    return run(kern[rounds - 1], (BULK ? 0 : kMaxRounds) + rounds - 1, 1, p, smem, st);
 }
 
 cudaError_t launch_distill(DistillArgs p, cudaStream_t st)
@@ -897,7 +947,7 @@ cudaError_t launch_distill(DistillArgs p, cudaStream_t st)
         if (smem <= kSmemLimit) break;
     }
     if (p.per < 64) return cudaErrorInvalidConfiguration;
-    return bulk ? run(k_distill_stream<true>, 2 * kMaxRounds, p, smem, st) : run(k_distill_stream<false>, 2 * kMaxRounds + 1, p, smem, st);
+    return bulk ? run(k_distill_stream<true>, 2 * kMaxRounds, 0, p, smem, st) : run(k_distill_stream<false>, 2 * kMaxRounds + 1, 0, p, smem, st);
 }
 
 }  // namespace
