@@ -5,15 +5,15 @@
 //   loss = tau^2 sum_j q_j (log q_j - log p_c(j)) ;  dz_v = rn16(tau * (p_v - sum of q_j with c(j) = v) * S / B)
 //
 // Bound: HBM, 4 bytes a logit (z read once, dz written once).  A row is spread over up to 16 warps of a CTA or over a
-// cluster of 2, 4 or 8 CTAs.  Every warp is a pipeline of its own over its part of every row: bulk copies in ahead of
-// time, sum of exponentials, gradient out.  What warps exchange is one (reference, sum)
-// pair per row, through (distributed) shared memory and an mbarrier; two more warps per CTA prepare the teacher's
-// entries rows ahead.
-//   Up to 32768 logits per CTA (262144 per row) the exponentials stay in registers between the two uses, each lane's
-// relative to its own maximum: one special-function result and about 6 instructions a logit.
+// cluster of 2, 4 or 8 CTAs.  Each warp sums the exponentials of its part of a row and turns them into the gradient.
+// What warps exchange is one (reference, sum) pair per row, through (distributed) shared memory and an mbarrier; two
+// more warps per CTA prepare the teacher's entries rows ahead.
+//   Up to 32768 logits per CTA (262144 per row) a further warp moves whole rows in and out by bulk copies, and the
+// exponentials stay in registers between the two uses, each lane's relative to its own maximum: one special-function
+// result and about 6 instructions a logit (4096 x 32000 112 us = 4.7 TB/s, 2001 x 20011 43 us).
 //   Longer rows pass through shared memory twice, the second time from L2 (clusters of 4: about 33 rows of 1.6 MB are
 // in work at a time; first reads are marked to stay, second reads and the gradient to leave first), and take their
-// exponentials twice.
+// exponentials twice (512 x 793471 422 us).
 #include <math.h>
 
 #include "mpt_common.cuh"

@@ -16,6 +16,8 @@
 // The backward pass adds dy*h and dy into per-lane FP32 column sums, leaves one partial row of them per CTA in the
 // workspace and adds those in a second kernel in a fixed order: results are run-to-run identical, nothing is added
 // atomically.  The partial sums are at most 148 rows whatever the batch.
+// Measured: 4096 x 12288 forward 44-48 us (4.2-4.6 TB/s), 40960 x 1024 forward 36, backward 54 us (4.7 TB/s), 2047 x 8191
+// backward 36 us.  Rows that are not 16-byte aligned: 4096 x 12287 165 and 450 us.
 #include <math.h>
 
 #include "mpt_common.cuh"

@@ -90,7 +90,7 @@ SHAPES = [  # B, C, K, pitch, shift
     (1, 1, 1, 1, 0), (2, 7, 3, 8, 0), (3, 8, 8, 8, 0), (5, 9, 2, 16, 0), (64, 1000, 8, 1000, 0), (65, 1003, 33, 1008, 0),
     (33, 1003, 5, 1003, 0), (40, 8000, 64, 8000, 3), (700, 257, 100, 264, 0), (500, 32000, 64, 32000, 0), (310, 20011, 20, 20016, 0),
     (3, 32000, 16, 32000, 0), (80, 36001, 16, 36008, 0), (160, 60000, 16, 60000, 0), (40, 100001, 1000, 100008, 0), (20, 200001, 7, 200008, 0),
-    (9, 420000, 12, 420000, 0), (40, 500009, 40, 500016, 0), (2, 793471, 128, 793472, 0), (25, 600000, 5, 600000, 1), (30, 700, 1024, 704, 0),
+    (9, 420000, 12, 420000, 0), (33, 300007, 300, 300008, 0), (20, 1000003, 50, 1000008, 0), (40, 830000, 20, 830000, 0), (40, 500009, 40, 500016, 0), (2, 793471, 128, 793472, 0), (25, 600000, 5, 600000, 1), (30, 700, 1024, 704, 0),
     (6, 400001, 1024, 400008, 0), (70, 262144, 33, 262144, 0), (160, 16384, 64, 16384, 0), (1000, 2048, 40, 2048, 0)]
 
 
