@@ -519,7 +519,7 @@ void mpt_lstm_destroy(mpt_lstm_ctx *ctx);
  * stream work has completed (calls that may overlap need one each).  Results are run-to-run identical.
  * Rows that are 16-byte aligned (base pointers, and pitches that are multiples of 8) move by bulk copies and 16-byte
  * stores, others element by element; rows of more than 12288 features are read more than once (by kernels that keep
- * nothing of a row on chip).  cols from 1 to 2^30.  Outputs must not overlap inputs (the same pointer is
+ * nothing of a row on chip).  cols from 1 to 2^30, rows from 0 to 2^30 (MPT_ERR_SHAPE otherwise).  Outputs must not overlap inputs (the same pointer is
  * refused).  rows == 0: forward does nothing, backward writes zero dgamma and dbeta.  The stream must belong to
  * the current device (the launch fails otherwise: MPT_ERR_CUDA).  Bytes moved per element: 4 forward, 6 backward. */
 int mpt_layernorm_forward(int rows, int cols, const uint16_t *x_dev, int ldx, const uint16_t *gamma16_dev,
@@ -559,7 +559,7 @@ int mpt_softmax_ce(const uint16_t *z_dev, int ldz, const int32_t *labels_dev, in
  * OR-ed with 1 if any dW is inf or NaN (section 3.2).  status_dev (may be null): one uint32 the caller has zeroed,
  * receives a time-out code if a bounded wait of a product kernel runs out (results are then invalid).
  * H must be a multiple of 8, the four matrices 16-byte aligned with pitches that are multiples of 8
- * (MPT_ERR_SHAPE otherwise; V and N are arbitrary, V at most MPT_LINEAR_CE_MAX_V).  Outputs must not overlap inputs.
+ * (MPT_ERR_SHAPE otherwise; V and N are arbitrary, V at most MPT_LINEAR_CE_MAX_V, N and H at most 2^30).  Outputs must not overlap inputs.
  * workspace: 256-byte aligned, mpt_linear_ce_workspace_bytes of the same N, V, H, row_block (want_dx, want_dW: whether
  * dx_dev, dW_dev will be given), owned by the caller and in use until the call's stream work has completed: calls
  * that may overlap, captured graphs among them, need one each.  The rows are worked on row_block at a time (a
@@ -587,7 +587,7 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
  * null (losses only; lddz is then ignored).  To mix with a hard label, call mpt_softmax_ce with the other share of S
  * and add the two gradients (mpt_add_f16).
  * status_dev (may be null): one uint32 the caller has zeroed, receives a time-out code if a bounded wait runs out
- * (results are then invalid).  z and dz must not overlap.  Any B >= 0, 1 <= C <= MPT_DISTILL_MAX_C, 1 <= K <=
+ * (results are then invalid).  z and dz must not overlap.  0 <= B <= 2^30, 1 <= C <= MPT_DISTILL_MAX_C, 1 <= K <=
  * MPT_DISTILL_MAX_K; tau > 0; rows that are 16-byte aligned move by bulk copies, others element by element.
  * Nothing is allocated and no workspace is needed.  Results are run-to-run identical.  Asynchronous on the stream,
  * which must belong to the current device.  Bytes moved per logit: 4. */

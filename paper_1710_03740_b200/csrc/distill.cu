@@ -64,6 +64,7 @@ constexpr int kAhead = 4;            // rows of its own a teacher warp asks for 
 constexpr int kMaxWarps = 16;        // warps that hold logits: few, so that what each does once per row stays small
 constexpr int kMaxRounds = 8;        // vectors a lane keeps in registers
 constexpr int kChunk = 256;          // vectors of a buffer where rows are streamed
+constexpr int kMaxBatch = 1 << 30;   // what is added to row indexes stays inside 32 bits
 constexpr uint32_t kNegInf16 = 0xFC00u;
 
 __device__ __forceinline__ float h2f(uint32_t h) { return __half2float(__ushort_as_half((unsigned short)h)); }
@@ -961,7 +962,7 @@ extern "C" int mpt_distill_topk(const uint16_t *z_dev, int ldz, int B, int C, co
 {
     if (!z_dev || !t16_dev || !idx_dev || !row_loss_dev || !loss_dev || z_dev == dz_dev) return MPT_ERR_INVALID_ARG;
     if (!(tau > 0.0f) || !isfinite(tau) || !isfinite(1.4426950408889634f / tau) || !isfinite(S)) return MPT_ERR_INVALID_ARG;
-    if (B < 0 || C < 1 || C > MPT_DISTILL_MAX_C || K < 1 || K > MPT_DISTILL_MAX_K) return MPT_ERR_SHAPE;
+    if (B < 0 || B > kMaxBatch || C < 1 || C > MPT_DISTILL_MAX_C || K < 1 || K > MPT_DISTILL_MAX_K) return MPT_ERR_SHAPE;
     if (ldz < C || (dz_dev && lddz < C) || ldt < K) return MPT_ERR_SHAPE;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e = cudaSuccess;

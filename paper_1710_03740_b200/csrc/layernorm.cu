@@ -703,7 +703,7 @@ __global__ void __launch_bounds__(256) k_ln_param_grad(const float *__restrict__
 }
 
 constexpr int kLnMaxParts = 148;      // partial rows of the column sums: one CTA on each SM
-constexpr int kLnMaxCols = 1 << 30;   // column indexes stay far inside 32 bits
+constexpr int kLnMaxSize = 1 << 30;   // rows and features: what is added to their indexes stays inside 32 bits
 
 int ln_colp(int cols) { return (cols + 7) / 8 * 8; }
 int ln_parts(int rows) { return rows < kLnMaxParts ? rows : kLnMaxParts; }
@@ -814,7 +814,7 @@ int mpt_layernorm_forward(int rows, int cols, const uint16_t *x_dev, int ldx, co
 {
     if (!x_dev || !gamma16_dev || !y_dev || x_dev == y_dev) return MPT_ERR_INVALID_ARG;
     if (!(eps >= 0.0f) || !isfinite(eps)) return MPT_ERR_INVALID_ARG;
-    if (rows < 0 || cols < 1 || cols > kLnMaxCols || ldx < cols || ldy < cols) return MPT_ERR_SHAPE;
+    if (rows < 0 || rows > kLnMaxSize || cols < 1 || cols > kLnMaxSize || ldx < cols || ldy < cols) return MPT_ERR_SHAPE;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (rows == 0) return MPT_OK;
     const LnFwd p = {rows, cols, 0, x_dev, (size_t)ldx, gamma16_dev, beta16_dev, eps, y_dev, (size_t)ldy, mean_dev, rstd_dev, status_dev};
@@ -824,7 +824,7 @@ int mpt_layernorm_forward(int rows, int cols, const uint16_t *x_dev, int ldx, co
 int mpt_layernorm_workspace_bytes(int rows, int cols, size_t *bytes_out)
 {
     if (!bytes_out) return MPT_ERR_INVALID_ARG;
-    if (rows < 0 || cols < 1 || cols > kLnMaxCols) return MPT_ERR_SHAPE;
+    if (rows < 0 || rows > kLnMaxSize || cols < 1 || cols > kLnMaxSize) return MPT_ERR_SHAPE;
     *bytes_out = (size_t)2 * (size_t)(ln_parts(rows) > 0 ? ln_parts(rows) : 1) * (size_t)ln_colp(cols) * sizeof(float);
     return MPT_OK;
 }
@@ -837,7 +837,7 @@ int mpt_layernorm_backward(int rows, int cols, const uint16_t *dy_dev, int lddy,
     if (!dy_dev || !x_dev || !gamma16_dev || !mean_dev || !rstd_dev || !dx_dev || !dgamma16_dev || !workspace_dev)
         return MPT_ERR_INVALID_ARG;
     if (dx_dev == dy_dev || dx_dev == x_dev) return MPT_ERR_INVALID_ARG;
-    if (rows < 0 || cols < 1 || cols > kLnMaxCols || lddy < cols || ldx < cols || lddx < cols) return MPT_ERR_SHAPE;
+    if (rows < 0 || rows > kLnMaxSize || cols < 1 || cols > kLnMaxSize || lddy < cols || ldx < cols || lddx < cols) return MPT_ERR_SHAPE;
     size_t need = 0;
     mpt_layernorm_workspace_bytes(rows, cols, &need);
     if (workspace_bytes < need || ((uintptr_t)workspace_dev & 15) != 0) return MPT_ERR_WORKSPACE;

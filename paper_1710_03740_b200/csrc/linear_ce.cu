@@ -29,6 +29,7 @@ namespace {
 constexpr int kGroup = 128;           // classes of one softmax group (CeEpi)
 constexpr float kLog2e = 1.4426950408889634f;      // as in the softmax epilogue
 constexpr int kDefaultRows = 4096;    // rows of a block when the caller does not choose
+constexpr int kMaxSize = 1 << 30;     // N and H: what is added to their indexes stays inside 32 bits
 constexpr int kMaxRows = 65536;       // largest block: CTAs of a pass over it stay inside 31 bits
 
 __device__ __forceinline__ float ex2(float x)
@@ -167,6 +168,12 @@ __global__ void __launch_bounds__(256) k_ce_rescale(uint16_t *__restrict__ e16, 
     }
 }
 
+bool bad_sizes(int N, int V, int H, int row_block)
+{
+    return N < 0 || N > kMaxSize || V < 1 || V > MPT_LINEAR_CE_MAX_V || H < 8 || H > kMaxSize || H % 8 || row_block < 0 ||
+           row_block > kMaxRows || row_block % 256;
+}
+
 // Where things are in the workspace (256-byte aligned offsets).
 struct Plan {
     int R, blocks;        // rows of a block, number of blocks
@@ -302,7 +309,7 @@ extern "C" {
 int mpt_linear_ce_workspace_bytes(int N, int V, int H, int want_dx, int want_dW, int row_block, size_t *bytes_out)
 {
     if (!bytes_out) return MPT_ERR_INVALID_ARG;
-    if (N < 0 || V < 1 || V > MPT_LINEAR_CE_MAX_V || H < 8 || H % 8 || row_block < 0 || row_block > kMaxRows || row_block % 256) return MPT_ERR_SHAPE;
+    if (bad_sizes(N, V, H, row_block)) return MPT_ERR_SHAPE;
     *bytes_out = make_plan(N, V, H, want_dx != 0, want_dW != 0, row_block).total;
     return MPT_OK;
 }
@@ -314,7 +321,7 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
 {
     if (!x_dev || !W_dev || !labels_dev || !row_loss_dev || !loss_dev || !workspace_dev) return MPT_ERR_INVALID_ARG;
     if (!isfinite(S) || dx_dev == x_dev || dW_dev == W_dev) return MPT_ERR_INVALID_ARG;
-    if (N < 0 || V < 1 || V > MPT_LINEAR_CE_MAX_V || H < 8 || H % 8 || row_block < 0 || row_block > kMaxRows || row_block % 256) return MPT_ERR_SHAPE;
+    if (bad_sizes(N, V, H, row_block)) return MPT_ERR_SHAPE;
     if (ldx < H || ldw < H || (dx_dev && lddx < H) || (dW_dev && lddw < H)) return MPT_ERR_SHAPE;
     const uintptr_t bits = (uintptr_t)x_dev | (uintptr_t)W_dev | (uintptr_t)dx_dev | (uintptr_t)dW_dev;
     if ((bits & 15) || ldx % 8 || ldw % 8 || (dx_dev && lddx % 8) || (dW_dev && lddw % 8)) return MPT_ERR_SHAPE;

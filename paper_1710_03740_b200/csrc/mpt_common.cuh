@@ -88,7 +88,7 @@ inline cudaError_t launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, siz
 __device__ __forceinline__ void mean_of_rows(const float *row_loss, int B, float *loss, double *red)
 {
     double acc = 0.0;
-    for (int i = threadIdx.x; i < B; i += 256) acc += (double)row_loss[i];
+    for (unsigned i = threadIdx.x; i < (unsigned)B; i += 256) acc += (double)row_loss[i];
     red[threadIdx.x] = acc;
     __syncthreads();
     for (int o = 128; o > 0; o >>= 1) {

@@ -30,7 +30,7 @@ def bwd(lib, **k):
 @pytest.mark.parametrize("change,code", [
     (dict(x=None), INVALID), (dict(gamma=None), INVALID), (dict(y=None), INVALID), (dict(y=P(256)), INVALID),
     (dict(eps=-1e-5), INVALID), (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID),
-    (dict(rows=-1), SHAPE), (dict(cols=0), SHAPE), (dict(ldx=63), SHAPE), (dict(ldy=63), SHAPE),
+    (dict(rows=-1), SHAPE), (dict(rows=(1 << 30) + 1), SHAPE), (dict(rows=2 ** 31 - 1), SHAPE), (dict(cols=0), SHAPE), (dict(ldx=63), SHAPE), (dict(ldy=63), SHAPE),
     (dict(cols=(1 << 30) + 1, ldx=(1 << 30) + 1, ldy=(1 << 30) + 1), SHAPE)])
 def test_forward_refuses(lib, change, code):
     assert fwd(lib, **change) == code
@@ -39,7 +39,7 @@ def test_forward_refuses(lib, change, code):
 @pytest.mark.parametrize("change,code", [
     (dict(dy=None), INVALID), (dict(x=None), INVALID), (dict(gamma=None), INVALID), (dict(mean=None), INVALID),
     (dict(rstd=None), INVALID), (dict(dx=None), INVALID), (dict(dgamma=None), INVALID), (dict(ws=None), INVALID),
-    (dict(dx=P(256)), INVALID), (dict(dx=P(512)), INVALID), (dict(rows=-1), SHAPE), (dict(cols=0), SHAPE), (dict(lddy=63), SHAPE),
+    (dict(dx=P(256)), INVALID), (dict(dx=P(512)), INVALID), (dict(rows=-1), SHAPE), (dict(rows=(1 << 30) + 1), SHAPE), (dict(cols=0), SHAPE), (dict(lddy=63), SHAPE),
     (dict(ldx=63), SHAPE), (dict(lddx=63), SHAPE), (dict(nbytes=4 * 64 * 8 - 1), WORKSPACE), (dict(ws=P(4100)), WORKSPACE)])
 def test_backward_refuses(lib, change, code):
     assert bwd(lib, **change) == code
@@ -53,6 +53,7 @@ def test_workspace_size(lib):
     assert big == binding.mpt_layernorm_workspace_bytes(1000, 12288) < 64 << 20          # bounded whatever the batch
     out = C.c_size_t(0)
     assert lib.mpt_layernorm_workspace_bytes(-1, 64, C.byref(out)) == SHAPE
+    assert lib.mpt_layernorm_workspace_bytes((1 << 30) + 1, 64, C.byref(out)) == SHAPE
     assert lib.mpt_layernorm_workspace_bytes(4, 0, C.byref(out)) == SHAPE
     assert lib.mpt_layernorm_workspace_bytes(4, 64, None) == INVALID
 

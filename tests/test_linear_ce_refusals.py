@@ -25,7 +25,7 @@ def call(lib, **k):
     (dict(x=None), INVALID), (dict(W=None), INVALID), (dict(labels=None), INVALID), (dict(row_loss=None), INVALID),
     (dict(loss=None), INVALID), (dict(ws=None), INVALID), (dict(S=float("nan")), INVALID), (dict(S=float("inf")), INVALID),
     (dict(dx=P(256)), INVALID), (dict(dW=P(512)), INVALID),
-    (dict(N=-1), SHAPE), (dict(V=0), SHAPE), (dict(V=(1 << 24) + 1), SHAPE), (dict(H=0), SHAPE), (dict(H=60), SHAPE), (dict(row_block=-256), SHAPE),
+    (dict(N=-1), SHAPE), (dict(N=(1 << 30) + 1), SHAPE), (dict(N=2 ** 31 - 1), SHAPE), (dict(H=(1 << 30) + 8, ldx=(1 << 30) + 8, ldw=(1 << 30) + 8), SHAPE), (dict(V=0), SHAPE), (dict(V=(1 << 24) + 1), SHAPE), (dict(H=0), SHAPE), (dict(H=60), SHAPE), (dict(row_block=-256), SHAPE),
     (dict(row_block=100), SHAPE), (dict(row_block=65536 + 256), SHAPE), (dict(ldx=56), SHAPE), (dict(ldw=56), SHAPE), (dict(lddx=56), SHAPE), (dict(lddw=56), SHAPE),
     (dict(ldx=68), SHAPE), (dict(ldw=68), SHAPE), (dict(lddx=68), SHAPE), (dict(lddw=68), SHAPE), (dict(x=P(264)), SHAPE),
     (dict(W=P(520)), SHAPE), (dict(dx=P(2056)), SHAPE), (dict(dW=P(4104)), SHAPE),
@@ -47,4 +47,6 @@ def test_workspace_size(lib):
         b.mpt_linear_ce_workspace_bytes(16, 32000, 1020)
     out = C.c_size_t(0)
     assert lib.mpt_linear_ce_workspace_bytes(4, 10, 64, 1, 1, 0, None) == INVALID
+    assert lib.mpt_linear_ce_workspace_bytes(2 ** 31 - 1, 10, 64, 1, 1, 0, C.byref(out)) == SHAPE
+    assert b.mpt_linear_ce_workspace_bytes(1 << 30, 10, 64) == b.mpt_linear_ce_workspace_bytes(8192, 10, 64)
     assert lib.mpt_linear_ce_workspace_bytes(4, 10, 64, 1, 1, 255, C.byref(out)) == SHAPE
