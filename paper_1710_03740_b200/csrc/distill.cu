@@ -961,7 +961,9 @@ extern "C" int mpt_distill_topk(const uint16_t *z_dev, int ldz, int B, int C, co
                                 float *loss_dev, uint32_t *status_dev, void *cuda_stream)
 {
     if (!z_dev || !t16_dev || !idx_dev || !row_loss_dev || !loss_dev || z_dev == dz_dev) return MPT_ERR_INVALID_ARG;
-    if (!(tau > 0.0f) || !isfinite(tau) || !isfinite(1.4426950408889634f / tau) || !isfinite(S)) return MPT_ERR_INVALID_ARG;
+    // 65504 log2(e) / tau stays below 2^31, where rounding an exponent's reference is off by 64: sums relative to it cannot
+    // overflow
+    if (!(tau >= 0x1p-14f && tau <= 0x1p14f) || !isfinite(S)) return MPT_ERR_INVALID_ARG;
     if (B < 0 || B > kMaxBatch || C < 1 || C > MPT_DISTILL_MAX_C || K < 1 || K > MPT_DISTILL_MAX_K) return MPT_ERR_SHAPE;
     if (ldz < C || (dz_dev && lddz < C) || ldt < K) return MPT_ERR_SHAPE;
     cudaStream_t st = (cudaStream_t)cuda_stream;

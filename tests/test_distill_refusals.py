@@ -24,7 +24,7 @@ def call(lib, **k):
 @pytest.mark.parametrize("change,code", [
     (dict(z=None), INVALID), (dict(t=None), INVALID), (dict(idx=None), INVALID), (dict(row_loss=None), INVALID), (dict(loss=None), INVALID),
     (dict(dz=P(256)), INVALID), (dict(tau=0.0), INVALID), (dict(tau=-1.0), INVALID), (dict(tau=float("nan")), INVALID),
-    (dict(tau=float("inf")), INVALID), (dict(tau=1e-45), INVALID), (dict(S=float("inf")), INVALID), (dict(S=float("nan")), INVALID),
+    (dict(tau=float("inf")), INVALID), (dict(tau=1e-45), INVALID), (dict(tau=6e-5), INVALID), (dict(tau=16400.0), INVALID), (dict(S=float("inf")), INVALID), (dict(S=float("nan")), INVALID),
     (dict(B=-1), SHAPE), (dict(B=(1 << 30) + 1), SHAPE), (dict(B=2 ** 31 - 1), SHAPE), (dict(C=0), SHAPE), (dict(C=(1 << 26) + 1, ldz=(1 << 26) + 1, lddz=(1 << 26) + 1), SHAPE), (dict(K=0), SHAPE),
     (dict(K=1025, ldt=1025), SHAPE), (dict(ldz=63), SHAPE), (dict(lddz=63), SHAPE), (dict(ldt=7), SHAPE)])
 def test_refusals(lib, change, code):

@@ -141,6 +141,35 @@ def test_extreme_logits(C):
 
 
 @pytest.mark.parametrize("C", [300, 32000, 500000])
+def test_smallest_temperature(C):
+    """tau = 2^-14: exponents of up to 1.5e9, which FP32 spaces 128 apart.  Logits that differ do so by at least 2^-9 / tau = 32,
+    so every p is 1 / (number of the row's largest logits) or below e^-32, and so is q."""
+    B, K, tau, S = 6, 5, 2.0 ** -14, 2.0 ** 20
+    rng = np.random.default_rng(C)
+    z, t, idx = make(B, C, K, 77 + C)
+    z = (rng.integers(-65504 // 32, 65504 // 32 + 1, (B, C)) * 32.0).astype(np.float16)
+    t = rng.integers(-8, 9, (B, K)).astype(np.float16)
+    z[1] = -65504.0
+    z[2, 5] = 65504.0
+    z[3] = np.where(np.arange(C) % 3 == 0, 65472.0, -65504.0)
+    z[4] = 1.5 - rng.integers(0, 2, C) / 512.0
+    dz, rl, loss = call(z, t, idx, tau, S)
+    top = z == z.max(1, keepdims=True)
+    p = top / top.sum(1, keepdims=True)
+    tt = t == t.max(1, keepdims=True)
+    q = tt / tt.sum(1, keepdims=True)
+    d = p.copy()
+    for r in range(B):
+        np.add.at(d[r], idx[r], -q[r])
+    c = tau * S / B
+    rel = (C / 256 + 200 + K) * U
+    e = c * ((rel + 2.0 ** -46) * (np.abs(d) + 2 * p) + 2.0 ** -46)
+    e = e + H16 * (np.abs(c * d) + e) + 2.0 ** -25
+    assert np.all(np.abs(dz.cpu().numpy() - c * d) <= e)
+    assert np.isfinite(loss) and bool(rl.isfinite().all())
+
+
+@pytest.mark.parametrize("C", [300, 32000, 500000])
 def test_nonfinite_values_stay_in_their_rows(C):
     z, t, idx = make(8, C, 6, 5 + C)
     z[1, 3] = np.nan
