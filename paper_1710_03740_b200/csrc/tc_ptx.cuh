@@ -677,8 +677,9 @@ __device__ __forceinline__ void epilogue_ce_group(uint32_t taddr, int col0, int 
             if ((unsigned)at < 32u) e.zlabel[row] = z;
         }
     }
-    // a group of nothing but -inf gets the exponent of a maximum of 0: its terms are zeros, not NaN
-    const float b = m == -INFINITY ? 14.0f : fmaf(-m, LOG2E, 14.0f);
+    // a group of nothing but -inf gets the exponent of a maximum of 0: its terms are zeros, not NaN.  b is rounded
+    // downwards: above 2^24 its steps are more than 1, and an exponential above 2^16 would be infinite in FP16
+    const float b = m == -INFINITY ? 14.0f : __fmaf_rd(-m, LOG2E, 14.0f);
     float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 1
     for (int c = 0; c < 4; c++) {

@@ -201,6 +201,60 @@ def test_large_logits():
     assert np.all(np.abs(got["dx"].cpu().numpy() - ref) <= tol + H16 * (np.abs(ref) + tol) + 2.0 ** -25)
 
 
+@pytest.mark.parametrize("N,V", [(40, 1000), (300, 30000)])
+def test_classes_masked_by_their_weights(N, V):
+    """Whole groups of classes whose first weight is FP16's lowest value, against a large positive feature: their logits are
+    about -6e7, their p is 0, and the losses and gradients are those of the other classes alone."""
+    x, W, y = make(N, V, 64, 19)
+    x[:, 0] = 1000.0 + np.arange(N) / 2
+    W[:, 0] = 0.0
+    masked = np.zeros(V, dtype=bool)
+    masked[100:700] = True
+    masked[V - 70:] = True
+    W[masked, 0] = -65504.0
+    keep = np.flatnonzero(~masked)
+    y = keep[np.random.default_rng(6).integers(0, len(keep), N)].astype(np.int32)
+    got = call(x, W, y, 128.0)
+    assert not got["dW"][torch.from_numpy(masked).cuda()].any() and got["flag"] == 0
+    got["dW"] = got["dW"][torch.from_numpy(~masked).cuda()]
+    check(x, W[keep], np.searchsorted(keep, y).astype(np.int32), 128.0, got)
+
+
+@pytest.mark.parametrize("N,V", [(24, 700), (260, 20000)])
+def test_logits_of_a_hundred_million(N, V):
+    """x . W = 1500 * 60000 + 8 * (0..3) * 2: exact in FP32 (multiples of 8 below 2^27), differences of 16 between classes.
+    FP32 spaces the exponents' reference 8 apart up there: the largest of a group is between 2^6 and 2^14, 2^-30 of it is
+    kept, and differences of 16 (2^-23.08 each) are exact, so p has the roundings of FP16 (normal numbers for the largest and
+    2^-24 absolute in its scale for the rest: 2^-29 of p at most)."""
+    H, S = 16, 256.0
+    rng = np.random.default_rng(V)
+    x, W = np.zeros((N, H), dtype=np.float16), np.zeros((V, H), dtype=np.float16)
+    x[:, 0], W[:, 0] = 1500.0, 60000.0
+    x[:, 1], W[:, 1] = 16.0, rng.integers(0, 4, V)
+    W[rng.integers(0, V, 5), 1] = 4.0
+    y = rng.integers(0, V, N).astype(np.int32)
+    got = call(x, W, y, S)
+    z = x.astype(np.float64) @ W.astype(np.float64).T
+    m = z.max(1, keepdims=True)
+    p = np.exp(z - m)
+    lse = m[:, 0] + np.log(p.sum(1))
+    p /= p.sum(1, keepdims=True)
+    d = p.copy()
+    d[np.arange(N), y] -= 1
+    rl = lse - z[np.arange(N), y]
+    assert np.all(np.abs(got["row_loss"].cpu().numpy() - rl) <= 1e-5 + 2.0 ** -20 * rl)
+    e = 2 * H16 * (1 + H16) * np.abs(d) + 1e-5 * p + 2.0 ** -28
+    M, X = W.astype(np.float64), x.astype(np.float64)
+    c = S / N
+    for name, ref, err, mag, K in (("dx", d @ M, e @ np.abs(M), np.abs(d) @ np.abs(M), V),
+                                   ("dW", d.T @ X, e.T @ np.abs(X), np.abs(d).T @ np.abs(X), N)):
+        g = got[name].cpu().numpy().astype(np.float64)
+        t = c * (err + (tc(K) + 4 * U) * mag)
+        t = t + H16 * (np.abs(c * ref) + t) + 2.0 ** -25
+        fits = np.abs(c * ref) + t < 65504
+        assert fits[:, 1:].all() and np.all(np.abs(g - c * ref)[fits] <= t[fits])
+
+
 def test_nonfinite_values_reach_what_they_must():
     x, W, y = make(40, 500, 64, 23)
     x[5, 1] = np.nan
@@ -259,6 +313,12 @@ def test_gradients_against_differences():
         # every d is within 3 * 2^-11 of its value, sums of at most 11 terms of size <= S/N * 3 each
         assert np.all(np.abs(g - num) <= 4 * H16 * (S / N) * 11 * 3)
         assert np.all(np.abs(g - num) <= 4 * H16 * np.abs(num) + 3e-2)
+
+
+def test_losses_ignore_the_scale():
+    x, W, y = make(70, 400, 64, 13)
+    a, b = call(x, W, y, float("nan"), "none"), call(x, W, y, 1.0, "none")
+    assert torch.equal(a["row_loss"], b["row_loss"]) and a["loss"] == b["loss"]
 
 
 def test_captured_and_replayed():

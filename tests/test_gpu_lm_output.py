@@ -177,3 +177,52 @@ def test_two_chains_at_once_give_what_they_give_alone():
     torch.cuda.synchronize()
     for c, ref in zip(chains, alone):
         assert all(torch.equal(a, r) for a, r in zip(c.outputs(), ref))
+
+
+FIRST_CALLS = """
+import torch
+from paper_1710_03740_b200 import binding as b
+torch.manual_seed(5)
+N, H, V, K, S = 300, 520, 20011, 12, 512.0
+f16 = lambda *s: torch.randn(*s, device="cuda").half()
+x, gamma, beta, W, t = f16(N, H), f16(H), f16(H), f16(V, H) * 0.05, f16(N, K)
+z = f16(N, 20016)
+y = torch.randint(0, V, (N,), device="cuda", dtype=torch.int32)
+idx = torch.randint(0, V, (N, K), device="cuda", dtype=torch.int32)
+h, dh, dx, dW, dz = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x), torch.empty_like(W), torch.empty_like(z)
+dg, db = torch.empty_like(gamma), torch.empty_like(beta)
+mean, rstd, rl, loss, rl2, loss2 = (torch.empty(n, device="cuda") for n in (N, N, N, 1, N, 1))
+wn = torch.empty(b.mpt_layernorm_workspace_bytes(N, H), dtype=torch.uint8, device="cuda")
+wl = torch.empty(b.mpt_linear_ce_workspace_bytes(N, V, H), dtype=torch.uint8, device="cuda")
+status = torch.zeros(1, dtype=torch.int32, device="cuda")
+outs = (h, dh, dx, dW, dz[:, :V], dg, db, mean, rstd, rl, loss, rl2, loss2)
+
+def run():
+    b.mpt_layernorm_forward(N, H, x, H, gamma, beta, 1e-5, h, H, mean, rstd, status)
+    b.mpt_linear_ce(N, V, H, h, H, W, H, y, S, rl, loss, dh, H, dW, H, wl, status=status)
+    b.mpt_layernorm_backward(N, H, dh, H, x, H, gamma, mean, rstd, dx, H, dg, db, wn, status=status)
+    b.mpt_distill_topk(z, 20016, N, V, t, idx, K, K, 2.0, S, dz, 20016, rl2, loss2, status)
+
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    run()
+for o in outs:
+    o.fill_(7.0)
+graph.replay()
+torch.cuda.synchronize()
+replayed = [o.clone() for o in outs]
+run()
+torch.cuda.synchronize()
+assert int(status) == 0
+assert all(torch.equal(a, o) for a, o in zip(replayed, outs))
+print("alike")
+"""
+
+
+def test_first_calls_of_a_process_are_captured():
+    """What a call sets up once per process and device is allowed while a stream is captured."""
+    import subprocess
+    import sys
+    from pathlib import Path
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], capture_output=True, text=True, timeout=300, cwd=Path(__file__).parents[1])
+    assert r.returncode == 0 and "alike" in r.stdout, r.stderr[-2000:]
