@@ -687,9 +687,9 @@ template <int R, bool BULK>
 __global__ void __launch_bounds__((kMaxWarps + kTeachers + 1) * 32, 1) k_distill(const DistillArgs p)
 {
     pdl_trigger();
-    pdl_wait();
     extern __shared__ __align__(128) uint8_t smem[];
     Cta<BULK, BULK> c(p, smem);
+    pdl_wait();                                       // up to here nothing was read or written that another kernel knows of
     if (c.warp >= p.nw) {
         if (c.warp < p.nw + kTeachers) c.teach();
         else if (BULK) c.move_rows();
@@ -779,9 +779,9 @@ template <bool BULK>
 __global__ void __launch_bounds__((kMaxWarps + kTeachers) * 32, 1) k_distill_stream(const DistillArgs p)
 {
     pdl_trigger();
-    pdl_wait();
     extern __shared__ __align__(128) uint8_t smem[];
     Cta<BULK, false> c(p, smem);
+    pdl_wait();                                       // up to here nothing was read or written that another kernel knows of
     if (c.warp >= p.nw) {
         c.teach();
         c.leave();

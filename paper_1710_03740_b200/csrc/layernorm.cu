@@ -7,17 +7,18 @@
 //             dgamma = rn16(sum over rows of dy * h) ;  dbeta = rn16(sum over rows of dy)
 //
 // Bound: HBM.  Forward reads x and writes y (4 bytes an element), backward reads dy and x and writes dx (6).
-// Up to 1024 features belong to one warp, longer rows (up to 12288 features) to as many warps of a CTA as that takes;
-// a warp keeps its features for all rows it works on, so the column sums of the parameter gradients stay in its registers.  Every warp is a pipeline of its own: its part of the next rows arrives in shared
-// memory by bulk copies while the present row is in registers (with all SMs' copies queued at the memory a load takes a
-// few microseconds, longer than a row), results leave by 16-byte stores.  The warps of a long row exchange their
-// sums through shared memory and a named barrier.  The variance is a second pass over the registers (sum of squared
-// deviations), not a difference of sums.
+// Up to 1024 features belong to one warp, longer rows (up to 16384 features, backward 12288) to as many warps of a CTA as
+// that takes; a warp keeps its features for all rows it works on, so the column sums of the parameter gradients stay in its
+// registers.  Every warp is a pipeline of its own: its part of the next rows arrives in shared memory by bulk copies while
+// the present row is in registers (with all SMs' copies queued at the memory a load takes a few microseconds, longer than a
+// row), results leave by 16-byte stores.  Scale and shift are in shared memory.  The warps of a long row exchange their sums
+// through shared memory and a named barrier.  The variance is a second pass over the registers (sum of squared deviations),
+// not a difference of sums.
 // The backward pass adds dy*h and dy into per-lane FP32 column sums, leaves one partial row of them per CTA in the
 // workspace and adds those in a second kernel in a fixed order: results are run-to-run identical, nothing is added
 // atomically.  The partial sums are at most 148 rows whatever the batch.
-// Measured: 4096 x 12288 forward 44-48 us (4.2-4.6 TB/s), 40960 x 1024 forward 36, backward 54 us (4.7 TB/s), 2047 x 8191
-// backward 36 us.  Rows that are not 16-byte aligned: 4096 x 12287 165 and 450 us.
+// Measured: 4096 x 12288 forward 45 us (4.5 TB/s), 40960 x 1024 forward 33 (5.1 TB/s), backward 52 us (4.8 TB/s), 2047 x 8191
+// backward 32 us.  Rows that are not 16-byte aligned: 4096 x 12287 199 and 440 us.
 #include <math.h>
 
 #include "mpt_common.cuh"
@@ -165,9 +166,23 @@ __device__ __forceinline__ void cta_sum2(float &a, float &b, float2 *red)
 
 // The work of one warp: features [8 v0, 8 (v0 + nv)) of the rows first, first + stride, ... (n of them), and the ring of
 // buffers through which NIN input matrices arrive.
-constexpr int kLnWarps = 12;          // warps of a CTA
-constexpr int kLnMaxRowWarps = 12;    // warps a row may take: 12288 features
-constexpr int kLnBuffers = 4;         // even: what follows their mbarriers is 16-byte aligned
+constexpr int kLnMaxRowWarps = 16;    // warps a row may take
+constexpr int kLnFwdWarps = 24;       // warps of a CTA of the forward kernel
+// Warps of a CTA of the backward kernel: as many as its column sums, 16 registers a vector, leave room for.
+constexpr __host__ __device__ int ln_bwd_warps(int R) { return R <= 2 ? 16 : 12; }
+// Buffers of a warp: as many as shared memory has room for beside the scale and shift vectors.
+constexpr __host__ __device__ int ln_buffers(int inputs) { return inputs == 1 ? 3 : 4; }
+// Shared memory of a CTA: buffers [warps][ln_buffers][inputs][32 R] of 16 bytes | the scale vector (forward: and the shift vector)
+// [row_warps][32 R] | mbarriers [warps][ln_buffers].
+constexpr __host__ __device__ uint32_t ln_params_at(int warps, int R, int inputs) { return (uint32_t)(warps * ln_buffers(inputs) * inputs * R * 512); }
+constexpr __host__ __device__ uint32_t ln_bars_at(int warps, int row_warps, int R, int inputs)
+{
+    return ln_params_at(warps, R, inputs) + (uint32_t)((inputs == 1 ? 2 : 1) * row_warps * R * 512);
+}
+constexpr __host__ __device__ uint32_t ln_smem(int warps, int row_warps, int R, int inputs)
+{
+    return ln_bars_at(warps, row_warps, R, inputs) + (uint32_t)(warps * ln_buffers(inputs) * 8);
+}
 
 template <int R, int NIN, bool BULK>
 struct LnWarp {
@@ -183,8 +198,8 @@ struct LnWarp {
     bool dead = false;
 
     static constexpr int kSlot = NIN * R * 32;      // vectors of a buffer
+    static constexpr int kBuffers = ln_buffers(NIN);
 
-    // shared memory: buffers [warps][kLnBuffers][NIN][32 R] of 16 bytes | mbarriers [warps][kLnBuffers] | the caller's
     __device__ __forceinline__ LnWarp(uint8_t *smem, int row_warps, int rows_, int cols_, volatile uint32_t *abort, uint32_t *status_)
     {
         warp = threadIdx.x >> 5;
@@ -201,12 +216,12 @@ struct LnWarp {
         first = (int)blockIdx.x * groups + g;
         stride = (int)gridDim.x * groups;
         n = first < rows ? (rows - 1 - first) / stride + 1 : 0;
-        buf = (uint4 *)smem + (size_t)warp * kLnBuffers * kSlot;
-        bar = smem_u32(smem + (size_t)warps * kLnBuffers * kSlot * 16) + 8u * (uint32_t)(warp * kLnBuffers);
+        buf = (uint4 *)smem + (size_t)warp * kBuffers * kSlot;
+        bar = smem_u32(smem + ln_bars_at(warps, nw, R, NIN)) + 8u * (uint32_t)(warp * kBuffers);
         abort_flag = abort;
         status = status_;
         if (lane == 0)
-            for (int s = 0; s < kLnBuffers; s++) mbar_init(bar + 8u * (uint32_t)s, 1);
+            for (int s = 0; s < kBuffers; s++) mbar_init(bar + 8u * (uint32_t)s, 1);
         if (threadIdx.x == 0) *abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -239,7 +254,7 @@ struct LnWarp {
             }
         }
         __syncwarp();
-        s_ask = s_ask + 1 == kLnBuffers ? 0 : s_ask + 1;
+        s_ask = s_ask + 1 == kBuffers ? 0 : s_ask + 1;
     }
     // Keeps the first `left` of eight values, zeros behind them.
     __device__ __forceinline__ static void clear_behind(uint4 &v, int left)
@@ -270,7 +285,7 @@ struct LnWarp {
             }
         }
         __syncwarp();
-        if (++s_use == kLnBuffers) {
+        if (++s_use == kBuffers) {
             s_use = 0;
             parity ^= 1u;
         }
@@ -303,6 +318,24 @@ struct LnWarp {
     __device__ __forceinline__ bool whole(int u) const { return BULK && (v0 + 32 * (u + 1)) * 8 <= cols; }
 };
 
+// A scale or shift vector (null: zeros) to shared memory, zeros from the last feature on; all loads are asked for before the
+// first is there.  Not inlined: its registers would be taken from the row loop's (4096 x 12288 forward 45 us, inlined 47.5).
+template <int R, bool BULK>
+__device__ __noinline__ void ln_params(uint4 *to, const uint16_t *from, int vectors, int cols)
+{
+    uint4 v[R];
+#pragma unroll
+    for (int u = 0; u < R; u++) {
+        const int col = ((int)threadIdx.x + u * (int)blockDim.x) * 8;
+        v[u] = from && col < cols ? load8<BULK, false>(from, col, cols) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int u = 0; u < R; u++) {
+        const int j = (int)threadIdx.x + u * (int)blockDim.x;
+        if (j < vectors) to[j] = v[u];
+    }
+}
+
 struct LnFwd {
     int rows, cols, row_warps;
     const uint16_t *x;
@@ -316,26 +349,35 @@ struct LnFwd {
 };
 
 template <int R, bool BULK>
-__global__ void __launch_bounds__(kLnWarps * 32, 2) k_ln_fwd(const LnFwd p)
+__global__ void __launch_bounds__(kLnFwdWarps * 32, 1) k_ln_fwd(const LnFwd p)
 {
     pdl_trigger();
-    pdl_wait();
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(16) float red[kLnWarps][2][16];
+    __shared__ __align__(16) float red[kLnFwdWarps / 2][2][16];      // a row of one warp has no use for it
     __shared__ uint32_t abort_word;
-    for (int i = threadIdx.x; i < kLnWarps * 32; i += blockDim.x) (&red[0][0][0])[i] = 0.0f;
+    for (int i = threadIdx.x; i < kLnFwdWarps * 16; i += blockDim.x) (&red[0][0][0])[i] = 0.0f;
     LnWarp<R, 1, BULK> c(smem, p.row_warps, p.rows, p.cols, &abort_word, p.status);
+    pdl_wait();                       // up to here nothing was read or written that another kernel knows of
     c.src[0] = p.x;
     c.ld[0] = p.ldx;
-    for (int i = 0; i < kLnBuffers; i++) c.request(i);
+    for (int i = 0; i < c.kBuffers; i++) c.request(i);
     const float inv_n = __fdiv_rn(1.0f, (float)p.cols);
     const int col0 = (c.v0 + c.lane) * 8;
+    // scale and shift in shared memory, zeros from the last feature on (48 KB of them for 12288 features do not stay in the L1
+    // that the buffers leave: read through it, every row waited for L2; 40960 x 1024 37 us, now 33)
+    const int vectors = c.nw * 32 * R;
+    uint4 *gamma = (uint4 *)(smem + ln_params_at((int)(blockDim.x >> 5), R, 1)), *beta = gamma + vectors;
+    ln_params<R, BULK>(gamma, p.gamma, vectors, p.cols);
+    ln_params<R, BULK>(beta, p.beta, vectors, p.cols);
+    __syncthreads();
+    gamma += c.v0 + c.lane;
+    beta += c.v0 + c.lane;
     auto rows = [&](auto whole) {
         constexpr bool W = decltype(whole)::value;
         for (int i = 0; i < c.n; i++) {
             uint4 x[1][R];
             c.template take<W>(x);
-            c.request(i + kLnBuffers);
+            c.request(i + c.kBuffers);
             f2 f[R][4];
             f2 s = pair(0.0f, 0.0f);
 #pragma unroll
@@ -379,13 +421,8 @@ __global__ void __launch_bounds__(kLnWarps * 32, 2) k_ln_fwd(const LnFwd p)
                 const bool whole_u = W || c.whole(u);
                 if (whole_u || col < p.cols) {
                     f2 g[4], b[4];
-                    if (whole_u) {                // these two stay in L1
-                        widen8(__ldg((const uint4 *)(p.gamma + col)), g);
-                        widen8(p.beta ? __ldg((const uint4 *)(p.beta + col)) : make_uint4(0u, 0u, 0u, 0u), b);
-                    } else {
-                        widen8(load8<BULK, false>(p.gamma, col, p.cols), g);
-                        widen8(p.beta ? load8<BULK, false>(p.beta, col, p.cols) : make_uint4(0u, 0u, 0u, 0u), b);
-                    }
+                    widen8(gamma[32 * u], g);
+                    widen8(beta[32 * u], b);
 #pragma unroll
                     for (int e = 0; e < 4; e++) f[u][e] = fma2(mul2(f[u][e], r2), g[e], b[e]);
                     if (whole_u) __stcs((uint4 *)(yr + 256 * u), round8(f[u]));
@@ -461,25 +498,24 @@ struct LnBwd {
 };
 
 template <int R, bool BULK>
-__global__ void __launch_bounds__(kLnWarps * 32, 1) k_ln_bwd(const LnBwd p)
+__global__ void __launch_bounds__(ln_bwd_warps(R) * 32, 1) k_ln_bwd(const LnBwd p)
 {
     pdl_trigger();
-    pdl_wait();
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(16) float red[kLnWarps][2][2][16];
+    __shared__ __align__(16) float red[8][2][2][16];       // a row of one warp has no use for it
     __shared__ uint32_t abort_word;
-    for (int i = threadIdx.x; i < kLnWarps * 64; i += blockDim.x) (&red[0][0][0][0])[i] = 0.0f;
+    for (int i = threadIdx.x; i < 8 * 64; i += blockDim.x) (&red[0][0][0][0])[i] = 0.0f;
     LnWarp<R, 2, BULK> c(smem, p.row_warps, p.rows, p.cols, &abort_word, p.status);
+    pdl_wait();                       // up to here nothing was read or written that another kernel knows of
     c.src[0] = p.x;
     c.ld[0] = p.ldx;
     c.src[1] = p.dy;
     c.ld[1] = p.lddy;
-    for (int i = 0; i < kLnBuffers; i++) c.request(i);
+    for (int i = 0; i < c.kBuffers; i++) c.request(i);
     const int col0 = (c.v0 + c.lane) * 8;
-    // gamma in shared memory, behind the mbarriers: zeros from the last feature on
-    uint4 *gamma = (uint4 *)(smem + (size_t)(blockDim.x >> 5) * kLnBuffers * (LnWarp<R, 2, BULK>::kSlot * 16 + 8));
-    for (int j = threadIdx.x; j < c.nw * 32 * R; j += blockDim.x)
-        gamma[j] = j * 8 < p.cols ? load8<BULK, false>(p.gamma, j * 8, p.cols) : make_uint4(0u, 0u, 0u, 0u);
+    // the scale in shared memory, zeros from the last feature on
+    uint4 *gamma = (uint4 *)(smem + ln_params_at((int)(blockDim.x >> 5), R, 2));
+    ln_params<R, BULK>(gamma, p.gamma, c.nw * 32 * R, p.cols);
     __syncthreads();
     gamma += c.v0 + c.lane;
     f2 ag[R][4], ab[R][4];
@@ -510,7 +546,7 @@ __global__ void __launch_bounds__(kLnWarps * 32, 1) k_ln_bwd(const LnBwd p)
             const f2 minus = pair(-mean, -mean), r2 = pair(rstd, rstd);
             uint4 v[2][R];
             c.template take<W>(v);
-            c.request(i + kLnBuffers);
+            c.request(i + c.kBuffers);
             f2 h[R][4], gy[R][4];
             f2 s1 = pair(0.0f, 0.0f), s2 = s1;
 #pragma unroll
@@ -563,41 +599,33 @@ __global__ void __launch_bounds__(kLnWarps * 32, 1) k_ln_bwd(const LnBwd p)
     if (c.whole(R - 1)) rows(Whole{});
     else rows(Ragged{});
     c.settle();
-    // the CTA's column sums; where several groups of warps hold the same features, added in group order
-    float *pg = p.parts + (size_t)blockIdx.x * p.colp, *pb = pg + (size_t)gridDim.x * p.colp;
-    const int groups = (int)(blockDim.x >> 5) / c.nw;
-    if (groups > 1) {
-        float *sums = (float *)smem;                     // [groups][nw * 256 R]: the buffers are not in use any more
-        const int width = c.nw * 256 * R;
+    // The CTA's column sums, through the ring's memory (not in use any more): a lane holds 8 neighbouring columns, and 8-byte
+    // stores 32 bytes apart took 7 us for 8191 features.  Several groups of warps that hold the same features are added in
+    // group order.
+    const int groups = (int)(blockDim.x >> 5) / c.nw, width = c.nw * 256 * R;
+    float *sums = (float *)smem;                     // [2][groups][width]
 #pragma unroll
-        for (int which = 0; which < 2; which++) {
-            __syncthreads();
+    for (int u = 0; u < R; u++) {
+        float4 *g = (float4 *)(sums + c.g * width + (c.v0 + c.lane + 32 * u) * 8), *b = g + groups * width / 4;
+        const float2 g0 = halves(ag[u][0]), g1 = halves(ag[u][1]), g2 = halves(ag[u][2]), g3 = halves(ag[u][3]);
+        const float2 b0 = halves(ab[u][0]), b1 = halves(ab[u][1]), b2 = halves(ab[u][2]), b3 = halves(ab[u][3]);
+        g[0] = make_float4(g0.x, g0.y, g1.x, g1.y);
+        g[1] = make_float4(g2.x, g2.y, g3.x, g3.y);
+        b[0] = make_float4(b0.x, b0.y, b1.x, b1.y);
+        b[1] = make_float4(b2.x, b2.y, b3.x, b3.y);
+    }
+    __syncthreads();
 #pragma unroll
-            for (int u = 0; u < R; u++) {
-                float4 *s = (float4 *)(sums + c.g * width + (c.v0 + c.lane + 32 * u) * 8);
-                f2 (&a)[4] = which ? ab[u] : ag[u];
-                const float2 a0 = halves(a[0]), a1 = halves(a[1]), a2 = halves(a[2]), a3 = halves(a[3]);
-                s[0] = make_float4(a0.x, a0.y, a1.x, a1.y);
-                s[1] = make_float4(a2.x, a2.y, a3.x, a3.y);
+    for (int which = 0; which < 2; which++) {
+        float *out = p.parts + ((size_t)which * gridDim.x + blockIdx.x) * p.colp;
+        const float *from = sums + which * groups * width;
+        for (int col = threadIdx.x * 4; col < p.colp; col += blockDim.x * 4) {       // colp is a multiple of 8 and at most width
+            float4 s = *(const float4 *)(from + col);
+            for (int k = 1; k < groups; k++) {
+                const float4 t = *(const float4 *)(from + k * width + col);
+                s = make_float4(s.x + t.x, s.y + t.y, s.z + t.z, s.w + t.w);
             }
-            __syncthreads();
-            for (int col = threadIdx.x; col < p.cols; col += blockDim.x) {
-                float s = sums[col];
-                for (int k = 1; k < groups; k++) s += sums[k * width + col];
-                (which ? pb : pg)[col] = s;
-            }
-        }
-    } else {
-#pragma unroll
-        for (int u = 0; u < R; u++) {
-            const int col = (c.v0 + c.lane + 32 * u) * 8;
-            if (col < p.cols) {                    // colp is a multiple of 8: a started vector is whole
-#pragma unroll
-                for (int e = 0; e < 4; e++) {
-                    *(float2 *)(pg + col + 2 * e) = halves(ag[u][e]);
-                    *(float2 *)(pb + col + 2 * e) = halves(ab[u][e]);
-                }
-            }
+            *(float4 *)(out + col) = s;
         }
     }
 }
@@ -666,25 +694,28 @@ __global__ void __launch_bounds__(256) k_ln_cols_long(const LnBwd p)
     }
     float *pg = p.parts + (size_t)blockIdx.y * p.colp, *pb = pg + (size_t)gridDim.y * p.colp;
 #pragma unroll
-    for (int e = 0; e < 8; e++) { pg[col + e] = ag[e]; pb[col + e] = ab[e]; }
+    for (int e = 0; e < 8; e += 4) {
+        *(float4 *)(pg + col + e) = make_float4(ag[e], ag[e + 1], ag[e + 2], ag[e + 3]);
+        *(float4 *)(pb + col + e) = make_float4(ab[e], ab[e + 1], ab[e + 2], ab[e + 3]);
+    }
 }
 
-// dgamma / dbeta: the partial rows added in a fixed order (eight warps take every eighth row, their sums are
+// dgamma / dbeta: the partial rows added in a fixed order (sixteen warps take every sixteenth row, their sums are
 // then added in warp order), rounded to FP16 and inspected for inf/NaN.  blockIdx.y: 0 dgamma, 1 dbeta.
-__global__ void __launch_bounds__(256) k_ln_param_grad(const float *__restrict__ parts, int nparts, int cols, int colp,
+__global__ void __launch_bounds__(512) k_ln_param_grad(const float *__restrict__ parts, int nparts, int cols, int colp,
                                                        uint16_t *__restrict__ dgamma, uint16_t *__restrict__ dbeta,
                                                        uint32_t *nonfinite_flag)
 {
     pdl_trigger();
     pdl_wait();
-    __shared__ float sh[8][32];
+    __shared__ float sh[16][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int col = blockIdx.x * 32 + lane;
     const float *src = parts + (size_t)blockIdx.y * nparts * colp;
     float s = 0.0f;
     if (col < cols) {
-#pragma unroll 4
-        for (int r = warp; r < nparts; r += 8) s += src[(size_t)r * colp + col];
+#pragma unroll 10
+        for (int r = warp; r < nparts; r += 16) s += src[(size_t)r * colp + col];
     }
     sh[warp][lane] = s;
     __syncthreads();
@@ -693,7 +724,7 @@ __global__ void __launch_bounds__(256) k_ln_param_grad(const float *__restrict__
         if (col < cols) {
             s = sh[0][lane];
 #pragma unroll
-            for (int w = 1; w < 8; w++) s += sh[w][lane];
+            for (int w = 1; w < 16; w++) s += sh[w][lane];
             const uint32_t h = (uint32_t)__half_as_ushort(__float2half_rn(s));
             bad = half_bits_nonfinite(h);
             (blockIdx.y ? dbeta : dgamma)[col] = (uint16_t)h;
@@ -709,27 +740,29 @@ int ln_colp(int cols) { return (cols + 7) / 8 * 8; }
 int ln_parts(int rows) { return rows < kLnMaxParts ? rows : kLnMaxParts; }
 
 // How rows of c8 vectors are laid over warps: R vectors a lane, row_warps warps a row, groups of them in a CTA (fewer
-// where there are not enough rows for all SMs), and the grid for `per_sm` CTAs of kLnWarps warps on an SM.
+// where there are not enough rows for all SMs), and the grid: one CTA with all warps on an SM, or as many
+// smaller ones as make that up.
 struct LnShape {
     int R, row_warps, groups, grid;
 };
-LnShape ln_shape(int rows, int c8, int per_sm)
+LnShape ln_shape(int rows, int c8, bool backward)
 {
-    // one warp a row where that is possible; else the R in 2..4 that leaves the fewest of kLnWarps warps without work
-    // (8191 features: 11 warps of 3 vectors a lane rather than 8 of 4), the larger where two are alike
-    LnShape s = {c8 <= 32 ? 1 : (c8 <= 64 ? 2 : 4), 0, 0, 0};
+    auto warps = [&](int r) { return backward ? ln_bwd_warps(r) : kLnFwdWarps; };
+    LnShape s = {c8 <= 128 ? (c8 + 31) / 32 : 4, 0, 0, 0};
     if (c8 > 128) {
         int best = 0;
         for (int r = 4; r >= 2; r--) {
-            const int w = (c8 + 32 * r - 1) / (32 * r), busy = w <= kLnWarps ? kLnWarps / w * w : 0;
+            const int w = (c8 + 32 * r - 1) / (32 * r), most = warps(r) < kLnMaxRowWarps ? warps(r) : kLnMaxRowWarps;
+            const int busy = w <= most ? warps(r) / w * w : 0;
             if (busy > best) { best = busy; s.R = r; }
         }
     }
+    const int all = warps(s.R);
     s.row_warps = (c8 + 32 * s.R - 1) / (32 * s.R);
-    const int most = kLnWarps / s.row_warps, spread = (rows + 147) / 148;
+    const int most = all / s.row_warps, spread = (rows + 147) / 148;
     s.groups = spread < most ? spread : most;
     const long ctas = ((long)rows + s.groups - 1) / s.groups;
-    const long fit = 148L * per_sm * (kLnWarps / (s.groups * s.row_warps));
+    const long fit = 148L * (all / (s.groups * s.row_warps));
     s.grid = (int)(ctas < fit ? ctas : fit);
     return s;
 }
@@ -741,10 +774,10 @@ cudaError_t ln_run(void (*kern)(const P), int id, const P &p, const LnShape &s, 
     const int dev = current_device_slot();
     if (dev < 0) return cudaErrorInvalidDevice;
     const int warps = s.groups * s.row_warps;
-    const size_t smem = (size_t)warps * kLnBuffers * ((size_t)inputs * s.R * 32 * 16 + 8) + (inputs == 2 ? (size_t)s.row_warps * s.R * 512 : 0);
+    const size_t smem = ln_smem(warps, s.row_warps, s.R, inputs);
     if (!configured[dev][id]) {
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                                   kLnWarps * kLnBuffers * (inputs * 4 * 32 * 16 + 8) + (inputs == 2 ? kLnWarps * 2048 : 0));
+        const int most = inputs == 1 ? ln_smem(kLnFwdWarps, kLnMaxRowWarps, 4, 1) : ln_smem(12, 12, 4, 2);
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
         if (e != cudaSuccess) return e;
         configured[dev][id] = true;
     }
@@ -758,7 +791,7 @@ cudaError_t launch_ln_fwd(LnFwd p, cudaStream_t st)
     const bool vec = (bits & 15) == 0 && ((p.ldx | p.ldy) & 7) == 0;
     const int c8 = (p.cols + 7) / 8;
     if (c8 <= kLnMaxRowWarps * 128) {
-        const LnShape s = ln_shape(p.rows, c8, 2);
+        const LnShape s = ln_shape(p.rows, c8, false);
         p.row_warps = s.row_warps;
         if (s.R == 1) return vec ? ln_run(k_ln_fwd<1, true>, 0, p, s, 1, st) : ln_run(k_ln_fwd<1, false>, 1, p, s, 1, st);
         if (s.R == 2) return vec ? ln_run(k_ln_fwd<2, true>, 2, p, s, 1, st) : ln_run(k_ln_fwd<2, false>, 3, p, s, 1, st);
@@ -778,8 +811,8 @@ cudaError_t launch_ln_bwd(LnBwd p, uint16_t *dgamma, uint16_t *dbeta, uint32_t *
     const int c8 = (p.cols + 7) / 8;
     int nparts = 0;
     cudaError_t e = cudaSuccess;
-    if (p.rows > 0 && c8 <= kLnMaxRowWarps * 128) {
-        const LnShape s = ln_shape(p.rows, c8, 1);
+    if (p.rows > 0 && c8 <= ln_bwd_warps(4) * 128) {
+        const LnShape s = ln_shape(p.rows, c8, true);
         p.row_warps = s.row_warps;
         nparts = s.grid;
         if (s.R == 1) e = vec ? ln_run(k_ln_bwd<1, true>, 0, p, s, 2, st) : ln_run(k_ln_bwd<1, false>, 1, p, s, 2, st);
@@ -797,7 +830,7 @@ cudaError_t launch_ln_bwd(LnBwd p, uint16_t *dgamma, uint16_t *dbeta, uint32_t *
     }
     if (e != cudaSuccess) return e;
     const dim3 grid((unsigned)((p.cols + 31) / 32), dbeta ? 2u : 1u);
-    MPT_LAUNCH(k_ln_param_grad, grid, dim3(256), 0, st, (const float *)p.parts, nparts, p.cols, p.colp, dgamma, dbeta, nonfinite_flag);
+    MPT_LAUNCH(k_ln_param_grad, grid, dim3(512), 0, st, (const float *)p.parts, nparts, p.cols, p.colp, dgamma, dbeta, nonfinite_flag);
     return cudaSuccess;
 }
 

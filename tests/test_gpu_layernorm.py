@@ -111,7 +111,7 @@ def ref_backward(dy, x, gamma, mean, rstd):
 SHAPES = [(1, 1, 1, 0), (1, 8, 8, 0), (3, 7, 7, 0), (5, 64, 64, 0), (64, 256, 256, 0), (33, 255, 256, 0), (9, 300, 301, 0),
           (150, 1000, 1000, 0), (17, 1024, 1032, 0), (1200, 1024, 1024, 0), (21, 1025, 1032, 0), (40, 2048, 2048, 0),
           (300, 4095, 4096, 0), (31, 6144, 6144, 0), (7, 6145, 6152, 0), (149, 12288, 12288, 0), (5, 12287, 12288, 0),
-          (12, 1024, 1024, 3), (6, 5000, 5001, 1), (3, 12296, 12296, 0), (2, 33000, 33000, 0), (5, 40001, 40001, 1)]
+          (12, 1024, 1024, 3), (6, 5000, 5001, 1), (3, 12296, 12296, 0), (300, 768, 768, 0), (160, 16384, 16384, 0), (33, 15001, 15008, 0), (3, 16392, 16392, 0), (600, 8184, 8192, 0), (2, 33000, 33000, 0), (5, 40001, 40001, 1)]
 
 
 @pytest.mark.parametrize("rows,cols,ld,shift", SHAPES)
