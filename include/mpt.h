@@ -591,7 +591,8 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
  * status_dev (may be null): one uint32 the caller has zeroed, receives a time-out code if a bounded wait runs out
  * (results are then invalid).  z and dz must not overlap.  0 <= B <= 2^30, 1 <= C <= MPT_DISTILL_MAX_C, 1 <= K <=
  * MPT_DISTILL_MAX_K; tau from 2^-14 to 2^14 (beyond, exponents of the largest FP16 logits, or tau^2 times a rounding, are not
- * resolved in FP32: MPT_ERR_INVALID_ARG); rows that are 16-byte aligned move by bulk copies, others element by element.
+ * resolved in FP32: MPT_ERR_INVALID_ARG); rows may lie to 16-byte boundaries as they like, if those of
+ * dz lie as those of z do (otherwise the gradient leaves element by element).
  * Nothing is allocated and no workspace is needed.  Results are run-to-run identical.  Asynchronous on the stream,
  * which must belong to the current device.  Bytes moved per logit: 4. */
 #define MPT_DISTILL_MAX_K 1024

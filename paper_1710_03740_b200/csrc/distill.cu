@@ -10,10 +10,11 @@
 // more warps per CTA prepare the teacher's entries rows ahead.
 //   Up to 32768 logits per CTA (262144 per row) a further warp moves whole rows in and out by bulk copies, and the
 // exponentials stay in registers between the two uses, each lane's relative to its own maximum: one special-function
-// result and about 6 instructions a logit (4096 x 32000 112 us = 4.7 TB/s, 2001 x 20011 43 us).
+// result and about 6 instructions a logit (4096 x 32000 109 us = 4.8 TB/s, 2001 x 20011 43 us, 4096 x 32001 without a pitch,
+// where every row lies differently to 16-byte boundaries, 119 us).
 //   Longer rows pass through shared memory twice, the second time from L2 (clusters of 4: about 33 rows of 1.6 MB are
 // in work at a time; first reads are marked to stay, second reads and the gradient to leave first), and take their
-// exponentials twice (512 x 793471 422 us).
+// exponentials twice (512 x 793471 416 us).
 #include <math.h>
 
 #include "mpt_common.cuh"
@@ -39,12 +40,22 @@ struct DistillArgs {
     uint32_t *kerr;
     int nw;              // warps that hold logits (kTeachers more prepare the teacher's entries)
     int wv;              // vectors of 8 logits per warp
+    int cv;              // vectors that a row may touch
     int vp;              // vectors per CTA
     int cl;              // CTAs per cluster
     int ns;              // buffers per warp
     int nb_log2;         // buffers for a row's entries: 2^nb_log2
     int per;             // vectors per buffer: wv, or a chunk of it where rows are streamed
+    int same;            // rows of dz lie to 16-byte boundaries as those of z do
 };
+
+// Rows are worked on in the 16-byte vectors that they lie in: vector g of row r holds classes 8 g - shift ... + 7, what lies
+// before class 0 and behind the last counts as -inf.  A SHIFT of zero for all rows is known at compile time.
+template <bool SHIFT>
+__device__ __forceinline__ int shift_of(const DistillArgs &p, int row)
+{
+    return SHIFT ? (int)((((uintptr_t)p.z >> 1) + (size_t)row * p.ldz) & 7) : 0;
+}
 
 // A row's teacher entries in shared memory, each array K long: class (-1: none), teacher's probability, the student's
 // logit (kept by the warp that holds it while the gradient takes its place), and the teacher's probability of the class
@@ -162,22 +173,23 @@ __device__ __forceinline__ float2 row_pair(const float2 *red, int pairs)
     return make_float2(E, wsum(s));
 }
 
-// Eight neighbouring gradients of a row to global memory, the first at class `first`.
-template <bool WHOLE>
-__device__ __forceinline__ void store8(uint16_t *dst, const uint4 v, int first, int C)
+// Eight neighbouring gradients of a row to global memory, the first of class `first`; whole: dst is 16-byte aligned
+// (always, unless SHIFT).
+template <bool SHIFT>
+__device__ __forceinline__ void store8(uint16_t *dst, const uint4 v, int first, int C, bool whole)
 {
-    if (WHOLE && first + 8 <= C) {
+    if ((!SHIFT || (whole && first >= 0)) && first + 8 <= C) {
         __stcs((uint4 *)dst, v);
         return;
     }
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int e = 0; e < 8; e++)
-        if (first + e < C) dst[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+        if ((unsigned)(first + e) < (unsigned)C) dst[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
 }
 // Gradient of n vectors, 2^(z k - x) * cs with cs = tau S / (B y), from shared memory to dst (class `first` on).
-template <int N, bool WHOLE>
-__device__ __forceinline__ void grad_store(const uint4 *v, uint16_t *dst, int first, int C, float k, float x, float cs)
+template <int N, bool SHIFT>
+__device__ __forceinline__ void grad_store(const uint4 *v, uint16_t *dst, int first, int C, bool whole, float k, float x, float cs)
 {
     uint4 in[N];
 #pragma unroll
@@ -191,20 +203,20 @@ __device__ __forceinline__ void grad_store(const uint4 *v, uint16_t *dst, int fi
             const float2 f = __half22float2(*(const __half2 *)&w[q]);
             o[q] = pack_f16x2(ex2_approx(fmaf(f.x, k, -x)) * cs, ex2_approx(fmaf(f.y, k, -x)) * cs);
         }
-        store8<WHOLE>(dst + 256 * u, make_uint4(o[0], o[1], o[2], o[3]), first + 256 * u, C);
+        store8<SHIFT>(dst + 256 * u, make_uint4(o[0], o[1], o[2], o[3]), first + 256 * u, C, whole);
     }
 }
-template <bool WHOLE>
-__device__ __forceinline__ void grad_vectors(const uint4 *v, int n, uint16_t *dst, int first, int C, float k, float2 pr, float cs)
+template <bool SHIFT>
+__device__ __forceinline__ void grad_vectors(const uint4 *v, int n, uint16_t *dst, int first, int C, bool whole, float k, float2 pr, float cs)
 {
     const int lane = threadIdx.x & 31;
     int base = 0;
-    for (; base + 128 <= n; base += 128) grad_store<4, WHOLE>(v + base + lane, dst + (base + lane) * 8, first + (base + lane) * 8, C, k, pr.x, cs);
+    for (; base + 128 <= n; base += 128) grad_store<4, SHIFT>(v + base + lane, dst + (base + lane) * 8, first + (base + lane) * 8, C, whole, k, pr.x, cs);
     if (base + 64 <= n) {
-        grad_store<2, WHOLE>(v + base + lane, dst + (base + lane) * 8, first + (base + lane) * 8, C, k, pr.x, cs);
+        grad_store<2, SHIFT>(v + base + lane, dst + (base + lane) * 8, first + (base + lane) * 8, C, whole, k, pr.x, cs);
         base += 64;
     }
-    for (int j = base + lane; j < n; j += 32) grad_store<1, WHOLE>(v + j, dst + j * 8, first + j * 8, C, k, pr.x, cs);
+    for (int j = base + lane; j < n; j += 32) grad_store<1, SHIFT>(v + j, dst + j * 8, first + j * 8, C, whole, k, pr.x, cs);
 }
 // The teacher's classes among the logits [first, first + count) that warp w holds at h: keep their logits ...
 __device__ __forceinline__ void keep_targets(const uint16_t *h, int first, int count, const Entries &ent, int w)
@@ -226,9 +238,10 @@ __device__ __forceinline__ void patch_targets(uint16_t *dst, int first, int coun
 }
 
 // Teacher's entries of a row, by one warp.  Entries whose class is outside [0, C) or whose logit is -inf have no part;
-// returns whether any has.  `rank`: which CTA of the cluster this is.  Classes named more than once are found with a hash table (open addressing, `slots` words, a
+// returns whether any has.  `rank`: which CTA of the cluster this is.
+// Classes named more than once are found with a hash table (open addressing, `slots` words, a
 // power of two and at least 2 K); only theirs are added up, over the entries in order.
-__device__ __forceinline__ bool prepare_entries(const DistillArgs &p, int row, int rank, const Entries &ent, int *table, int slots)
+__device__ __forceinline__ bool prepare_entries(const DistillArgs &p, int row, int rank, int shift, const Entries &ent, int *table, int slots)
 {
     const int lane = threadIdx.x & 31;
     const int32_t *id = p.idx + (size_t)row * p.ldt;
@@ -253,7 +266,7 @@ __device__ __forceinline__ bool prepare_entries(const DistillArgs &p, int row, i
     bool twice = false;
     // the warp of this CTA that holds class v, kMaxWarps: none
     auto holder = [&](int v) {
-        const int at = (v >> 3) - rank * p.vp;
+        const int at = ((v + shift) >> 3) - rank * p.vp;
         return v >= 0 && at >= 0 && at < p.vp ? at / p.wv : kMaxWarps;
     };
     for (int j = lane; j < p.K; j += 32) {
@@ -397,11 +410,10 @@ static __device__ __noinline__ bool wait_asleep(uint32_t bar, uint32_t parity, v
     }
 }
 
-// What all warps of a CTA share, and each warp's part of the rows.  BULK: rows start on 16-byte boundaries and move by
-// bulk copies; otherwise the warps copy elements.  ROWS: the CTA's part of a row lies in one buffer of [ns] and moves as one
-// copy, in and out, by a warp that does nothing else: what a warp spends on issuing its own copies it spends once a row, and
-// all others wait for the slowest.  Otherwise each warp has ns buffers of its own.
-template <bool BULK, bool ROWS>
+// What all warps of a CTA share, and each warp's part of the rows.  ROWS: the CTA's part of a row lies in one buffer of [ns]
+// and moves as one copy, in and out, by a warp that does nothing else: what a warp spends on issuing its own copies it spends
+// once a row, and all others wait for the slowest.  Otherwise each warp has ns buffers of its own.
+template <bool SHIFT, bool ROWS>
 struct Cta {
     const DistillArgs &p;
     uint8_t *smem;
@@ -427,7 +439,7 @@ struct Cta {
         pairs = p.cl * p.nw;
         bars = smem_u32(smem + L.bars);
         abort_flag = (volatile uint32_t *)(smem + L.abort);
-        const int v_end = min((p.C + 7) / 8, (rank + 1) * p.vp);
+        const int v_end = min(p.cv, (rank + 1) * p.vp);
         v0 = rank * p.vp + warp * p.wv;
         nv = warp < p.nw ? max(0, min(v_end, v0 + p.wv) - v0) : 0;
         if (nv == 0) v0 = 0;
@@ -480,81 +492,79 @@ struct Cta {
             dead = true;
         }
     }
-    // Whole vectors among [f, f + n) of this warp's part as the copy of row i takes them.  A last, partial vector comes with
-    // what the pitch leaves behind it (mend() replaces that), but for the matrix's last row, whose memory may end with it.
-    __device__ __forceinline__ int copied(int i, int f, int n) const
-    {
-        return row_of(i) == p.B - 1 ? min(n, p.C / 8 - (v0 + f)) : n;
-    }
-    // Logits behind the last class become -inf (nothing to do unless the part ends in a partial vector).
+    __device__ __forceinline__ int shift(int i) const { return shift_of<SHIFT>(p, row_of(i)); }
+    // The class of the first element of this warp's part of row i.
+    __device__ __forceinline__ int first_class(int i) const { return v0 * 8 - shift(i); }
+    // What lies before the row's first class or behind its last becomes -inf, in vectors [f, f + n) of this warp's part.
     __device__ __forceinline__ void mend(int i, int s, int f, int n)
     {
-        if (BULK && (v0 + f + n) * 8 > p.C) {
-            if (copied(i, f, n) == n && lane < 8 && (v0 + f + n - 1) * 8 + lane >= p.C)
-                ((uint16_t *)(buf + s * pitch + n - 1))[lane] = (uint16_t)kNegInf16;
+        const int sh = shift(i), g0 = v0 + f;
+        uint16_t *h = (uint16_t *)(buf + s * pitch);
+        if (SHIFT && g0 == 0 && lane < sh) h[lane] = (uint16_t)kNegInf16;
+        if ((g0 + n) * 8 - sh > p.C) {               // the last vector, with a shift perhaps one more
+            for (int g = SHIFT ? max((p.C + sh) / 8, g0) : g0 + n - 1; g < g0 + n; g++)
+                if (lane < 8 && g * 8 - sh + lane >= p.C) h[(g - g0) * 8 + lane] = (uint16_t)kNegInf16;
             __syncwarp();
+        } else if (SHIFT && g0 == 0) __syncwarp();
+    }
+    // Vectors [first, first + n) of row i to dst, which is free; `bar` completes a phase with them.  A vector that is not the
+    // row's alone comes with what lies beside the row (mend() replaces that); one that reaches out of the matrix's memory,
+    // by elements.
+    __device__ __forceinline__ void bring(int i, uint4 *dst, int first, int n, uint32_t bar, uint64_t policy)
+    {
+        const int row = row_of(i), sh = shift(i);
+        const uint16_t *src = p.z + (size_t)row * p.ldz;
+        int a = 0, b = n;
+        if (SHIFT) {
+            const int lo = (size_t)row * p.ldz < (size_t)sh ? 1 : 0;
+            const int hi = (p.C + sh + ((size_t)(p.B - 1 - row) * p.ldz >= 7 ? 7 : 0)) / 8;
+            a = min(max(lo - first, 0), n);
+            b = max(min(hi - first, n), a);
+        } else if (row == p.B - 1) b = max(min(n, p.C / 8 - first), 0);
+        auto elements = [&](int g) {
+            const int c = (first + g) * 8 - sh + lane;
+            if (lane < 8) ((uint16_t *)(dst + g))[lane] = (unsigned)c < (unsigned)p.C ? src[c] : (uint16_t)kNegInf16;
+        };
+        if (a > 0 || b < n) {
+            for (int g = 0; g < a; g++) elements(g);
+            for (int g = b; g < n; g++) elements(g);
+            __syncwarp();                            // the arrival below tells of these, too
         }
+        if (lane == 0) {
+            if (b > a) bulk_in(smem_u32(dst + a), src + ((ptrdiff_t)(first + a) * 8 - sh), (uint32_t)(b - a) * 16u, bar, policy);
+            else mbar_arrive(bar);
+        }
+        __syncwarp();
     }
     // Requests vectors [f, f + n) of this warp's part of row i into buffer s (the caller knows that it is free).
     __device__ __forceinline__ void request(int i, int s, int f, int n, uint64_t policy)
     {
-        const uint16_t *src = p.z + (size_t)row_of(i) * p.ldz + (size_t)(v0 + f) * 8;
-        uint4 *dst = buf + s * pitch;
-        if (BULK) {
-            const int whole = copied(i, f, n);
-            if (lane == 0) {                                          // each use of a buffer completes one phase of its barrier
-                if (whole > 0) bulk_in(smem_u32(dst), src, (uint32_t)whole * 16u, bar0 + 8u * (uint32_t)s, policy);
-                else mbar_arrive(bar0 + 8u * (uint32_t)s);
-            }
-            if (whole < n && lane < 8) {
-                const int e = (v0 + f + whole) * 8 + lane;
-                ((uint16_t *)(dst + whole))[lane] = e < p.C ? src[whole * 8 + lane] : (uint16_t)kNegInf16;
-            }
-        } else {
-            for (int e = lane; e < n * 8; e += 32)
-                ((uint16_t *)dst)[e] = (v0 + f) * 8 + e < p.C ? src[e] : (uint16_t)kNegInf16;
-        }
-        __syncwarp();
+        bring(i, buf + s * pitch, v0 + f, n, bar0 + 8u * (uint32_t)s, policy);
     }
-    __device__ __forceinline__ void arrived(int s, uint32_t parity)
-    {
-        if (BULK) wait<false>(bar0 + 8u * (uint32_t)s, parity);
-    }
+    __device__ __forceinline__ void arrived(int s, uint32_t parity) { wait<false>(bar0 + 8u * (uint32_t)s, parity); }
     // ROWS: the work of the last warp.  Every buffer goes round: a row arrives, its gradient takes its place, leaves, and the
     // row ns further arrives.
     __device__ __forceinline__ void move_rows()
     {
         const uint64_t policy = l2_policy(2);        // every byte is used once
-        const int first = rank * p.vp, n = max(0, min((p.C + 7) / 8, first + p.vp) - first);
-        auto bring = [&](int i, int s) {
-            const uint16_t *src = p.z + (size_t)row_of(i) * p.ldz + (size_t)first * 8;
-            uint4 *dst = (uint4 *)smem + s * pitch;
-            // a partial vector at the row's end as in copied()
-            const int whole = row_of(i) == p.B - 1 ? min(n, p.C / 8 - first) : n;
-            if (whole < n && lane < 8) {
-                const int e = (first + whole) * 8 + lane;
-                ((uint16_t *)(dst + whole))[lane] = e < p.C ? src[whole * 8 + lane] : (uint16_t)kNegInf16;
-            }
-            __syncwarp();                            // the arrival below tells of these, too
-            if (lane == 0) {
-                if (whole > 0) bulk_in(smem_u32(dst), src, (uint32_t)whole * 16u, bar0 + 8u * (uint32_t)s, policy);
-                else mbar_arrive(bar0 + 8u * (uint32_t)s);
-            }
-        };
-        for (int i = 0; i < p.ns && i < n_rows; i++) bring(i, i);
+        const int first = rank * p.vp, n = max(0, min(p.cv, first + p.vp) - first);
+        auto fetch = [&](int i, int s) { bring(i, (uint4 *)smem + s * pitch, first, n, bar0 + 8u * (uint32_t)s, policy); };
+        for (int i = 0; i < p.ns && i < n_rows; i++) fetch(i, i);
         int s = 0;
         uint32_t parity = 0;
         for (int i = 0; i < n_rows; i++) {
             wait<false>(written_bar(s), parity);
             if (p.dz && lane == 0) {
-                const int whole = min(n, p.C / 8 - first);      // the owner of a partial vector stores its elements itself
-                if (whole > 0 && !dead)
-                    bulk_out(p.dz + (size_t)row_of(i) * p.lddz + (size_t)first * 8, smem_u32((uint4 *)smem + s * pitch), (uint32_t)whole * 16u, policy);
+                // the row's own vectors; the owner of a vector that it shares stores its elements itself
+                const int sh = shift(i), a = max(sh > 0 ? 1 : 0, first), b = min((p.C + sh) / 8, first + n);
+                if (b > a && p.same && !dead)
+                    bulk_out(p.dz + (size_t)row_of(i) * p.lddz + ((size_t)a * 8 - sh), smem_u32((uint4 *)smem + s * pitch + (a - first)),
+                             (uint32_t)(b - a) * 16u, policy);
                 bulk_commit_group();
                 bulk_wait_group_read<0>();
             }
             __syncwarp();
-            if (i + p.ns < n_rows) bring(i + p.ns, s);
+            if (i + p.ns < n_rows) fetch(i + p.ns, s);
             if (++s == p.ns) {
                 s = 0;
                 parity ^= 1u;
@@ -565,10 +575,17 @@ struct Cta {
     __device__ __forceinline__ void written(int i, int s)
     {
         if (p.dz) {
-            const int whole = min(nv, p.C / 8 - v0);
-            if (nv > 0 && whole < nv && lane < 8 && !dead) {
-                const int e = (v0 + whole) * 8 + lane;
-                if (e < p.C) out(i)[whole * 8 + lane] = ((const uint16_t *)(buf + s * pitch + whole))[lane];
+            if (SHIFT && !p.same) send(i, s);
+            else if (nv > 0 && !dead && (SHIFT || (v0 + nv) * 8 > p.C)) {
+                __syncwarp();                        // all lanes' gradients are there
+                const int sh = shift(i), last = (p.C + sh) / 8;
+                auto elements = [&](int g) {
+                    if (g < v0 || g >= v0 + nv || lane >= 8) return;
+                    const int c = g * 8 - sh + lane;
+                    if ((unsigned)c < (unsigned)p.C) (p.dz + (size_t)row_of(i) * p.lddz)[c] = ((const uint16_t *)(buf + s * pitch + (g - v0)))[lane];
+                };
+                if (SHIFT && sh > 0) elements(0);
+                if (last > 0 || sh == 0) elements(last);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
@@ -578,20 +595,21 @@ struct Cta {
     // Writes this warp's gradient of row i from buffer s, element by element.
     __device__ __forceinline__ void send(int i, int s)
     {
-        uint16_t *dst = out(i);
-        const uint4 *src = buf + s * pitch;
+        uint16_t *dst = p.dz + (size_t)row_of(i) * p.lddz;
+        const uint16_t *src = (const uint16_t *)(buf + s * pitch);
+        const int first = first_class(i);
         __syncwarp();
         if (!dead)
             for (int e = lane; e < nv * 8; e += 32)
-                if (v0 * 8 + e < p.C) dst[e] = ((const uint16_t *)src)[e];
+                if ((unsigned)(first + e) < (unsigned)p.C) dst[first + e] = src[e];
         __syncwarp();
     }
-    // Where this warp's gradient of row i goes.
-    __device__ __forceinline__ uint16_t *out(int i) const { return p.dz + (size_t)row_of(i) * p.lddz + (size_t)v0 * 8; }
+    // Where this warp's gradient of row i goes (its first vector's place, which may begin before the row).
+    __device__ __forceinline__ uint16_t *out(int i) const { return p.dz + (ptrdiff_t)((size_t)row_of(i) * p.lddz) + first_class(i); }
     // Zeros for this warp's part of a row without a teacher.
     __device__ __forceinline__ void send_zeros(int i)
     {
-        for (int j = lane; j < nv; j += 32) store8<BULK>(out(i) + j * 8, make_uint4(0u, 0u, 0u, 0u), (v0 + j) * 8, p.C);
+        for (int j = lane; j < nv; j += 32) store8<SHIFT>(out(i) + j * 8, make_uint4(0u, 0u, 0u, 0u), first_class(i) + j * 8, p.C, p.same);
     }
     // This warp's pair of row i to every CTA of the cluster.
     __device__ __forceinline__ void publish(int i, float2 pr)
@@ -658,7 +676,7 @@ struct Cta {
                 if (i == me)
                     for (int r = 1; r < kAhead; r++) prefetch_list(i + r * kTeachers);
                 prefetch_list(i + kAhead * kTeachers);
-                const bool any = prepare_entries(p, row_of(i), rank, entries(b), (int *)(smem + L.table) + me * L.slots, L.slots);
+                const bool any = prepare_entries(p, row_of(i), rank, shift(i), entries(b), (int *)(smem + L.table) + me * L.slots, L.slots);
                 if (lane == 0) {
                     *live(b) = any ? 1 : 0;
                     mbar_arrive(full_bar(b));
@@ -683,29 +701,22 @@ struct Cta {
 };
 
 // Rows whose exponentials stay in registers: R vectors per lane.
-template <int R, bool BULK>
+template <int R, bool SHIFT>
 __global__ void __launch_bounds__((kMaxWarps + kTeachers + 1) * 32, 1) k_distill(const DistillArgs p)
 {
     pdl_trigger();
     extern __shared__ __align__(128) uint8_t smem[];
-    Cta<BULK, BULK> c(p, smem);
+    Cta<SHIFT, true> c(p, smem);
     pdl_wait();                                       // up to here nothing was read or written that another kernel knows of
     if (c.warp >= p.nw) {
         if (c.warp < p.nw + kTeachers) c.teach();
-        else if (BULK) c.move_rows();
+        else c.move_rows();
         c.leave();
         return;
     }
     const int nv = c.nv;
-    int s_ask = 0, s_use = 0;
+    int s_use = 0;
     uint32_t parity = 0;
-    auto ask = [&](int i) {
-        if (!BULK && nv > 0 && i < c.n_rows) {
-            c.request(i, s_ask, 0, nv, 0);
-            s_ask = s_ask + 1 == p.ns ? 0 : s_ask + 1;
-        }
-    };
-    for (int i = 0; i + 1 < p.ns; i++) ask(i);
     for (int i = 0; i < c.n_rows; i++) {
         uint4 *v = c.buf + s_use * c.pitch;
         float e[R][8];
@@ -740,7 +751,7 @@ __global__ void __launch_bounds__((kMaxWarps + kTeachers + 1) * 32, 1) k_distill
         c.publish(i, warp_pair(m == -INFINITY ? -INFINITY : -b, s));
         const int eb = c.open_entries(i);
         const Entries ent = c.entries(eb);
-        if (nv > 0) keep_targets((const uint16_t *)v, c.v0 * 8, nv * 8, ent, c.warp);
+        if (nv > 0) keep_targets((const uint16_t *)v, c.first_class(i), nv * 8, ent, c.warp);
         __syncwarp();
         const float2 pr = c.collect(i);
         if (p.dz && nv > 0) {
@@ -756,14 +767,12 @@ __global__ void __launch_bounds__((kMaxWarps + kTeachers + 1) * 32, 1) k_distill
                                           pack_f16x2(e[u][4] * k, e[u][5] * k), pack_f16x2(e[u][6] * k, e[u][7] * k));
                 }
                 __syncwarp();
-                patch_targets((uint16_t *)v, c.v0 * 8, nv * 8, ent, c.warp, p.k, pr, cs, p.c);
+                patch_targets((uint16_t *)v, c.first_class(i), nv * 8, ent, c.warp, p.k, pr, cs, p.c);
             } else {
                 for (int j = c.lane; j < nv; j += 32) v[j] = make_uint4(0u, 0u, 0u, 0u);
             }
         }
-        if (BULK) c.written(i, s_use);
-        else if (p.dz && nv > 0) c.send(i, s_use);
-        ask(i + p.ns - 1);
+        c.written(i, s_use);
         c.close_entries(eb, pr);
         if (++s_use == p.ns) {
             s_use = 0;
@@ -775,12 +784,12 @@ __global__ void __launch_bounds__((kMaxWarps + kTeachers + 1) * 32, 1) k_distill
 
 // Rows that are read twice.  Chunks of this warp's part go through a ring of ns buffers in the order in which they are
 // used, first pass and second pass of one row after the other, requested ns - 1 ahead.
-template <bool BULK>
+template <bool SHIFT>
 __global__ void __launch_bounds__((kMaxWarps + kTeachers) * 32, 1) k_distill_stream(const DistillArgs p)
 {
     pdl_trigger();
     extern __shared__ __align__(128) uint8_t smem[];
-    Cta<BULK, false> c(p, smem);
+    Cta<SHIFT, false> c(p, smem);
     pdl_wait();                                       // up to here nothing was read or written that another kernel knows of
     if (c.warp >= p.nw) {
         c.teach();
@@ -836,11 +845,11 @@ __global__ void __launch_bounds__((kMaxWarps + kTeachers) * 32, 1) k_distill_str
                 ask();
                 c.arrived(s_use, parity);
                 c.mend(i, s_use, ch * per, min(per, nv - ch * per));
-                const int n = min(per, nv - ch * per), first = (c.v0 + ch * per) * 8;
+                const int n = min(per, nv - ch * per), first = c.first_class(i) + ch * per * 8;
                 const uint4 *v = c.buf + s_use * per;
                 uint16_t *dst = c.out(i) + ch * per * 8;
                 if (alive && !c.dead) {
-                    grad_vectors<BULK>(v, n, dst, first, p.C, p.k, pr, cs);
+                    grad_vectors<SHIFT>(v, n, dst, first, p.C, p.same, p.k, pr, cs);
                     keep_targets((const uint16_t *)v, first, n * 8, ent, c.warp);
                     __syncwarp();              // orders the warp's stores: the targets' come after those around them
                     patch_targets(dst, first, n * 8, ent, c.warp, p.k, pr, cs, p.c);
@@ -909,18 +918,21 @@ cudaError_t run(DistillKernel kern, int id, int extra, const DistillArgs &p, uin
     return cudaLaunchKernelEx(&cfg, kern, p);
 }
 
-template <bool BULK>
+template <bool SHIFT>
 cudaError_t launch_rounds(int rounds, const DistillArgs &p, uint32_t smem, cudaStream_t st)
 {
-    static const DistillKernel kern[kMaxRounds] = {k_distill<1, BULK>, k_distill<2, BULK>, k_distill<3, BULK>, k_distill<4, BULK>,
-                                                   k_distill<5, BULK>, k_distill<6, BULK>, k_distill<7, BULK>, k_distill<8, BULK>};
-    return run(kern[rounds - 1], (BULK ? 0 : kMaxRounds) + rounds - 1, 1, p, smem, st);
+    static const DistillKernel kern[kMaxRounds] = {k_distill<1, SHIFT>, k_distill<2, SHIFT>, k_distill<3, SHIFT>, k_distill<4, SHIFT>,
+                                                   k_distill<5, SHIFT>, k_distill<6, SHIFT>, k_distill<7, SHIFT>, k_distill<8, SHIFT>};
+    return run(kern[rounds - 1], (SHIFT ? kMaxRounds : 0) + rounds - 1, 1, p, smem, st);
 }
 
 cudaError_t launch_distill(DistillArgs p, cudaStream_t st)
 {
     const bool bulk = (((uintptr_t)p.z | (uintptr_t)p.dz) & 15) == 0 && (p.ldz & 7) == 0 && (!p.dz || (p.lddz & 7) == 0);
-    const int cv = (p.C + 7) / 8;
+    // another pitch or base: the vectors' borders lie elsewhere in every row (all C may be touched by one vector more), and where
+    // they lie elsewhere in dz, too, the gradient leaves by elements
+    p.same = !p.dz || ((((uintptr_t)p.z ^ (uintptr_t)p.dz) & 15) == 0 && ((p.ldz ^ p.lddz) & 7) == 0);
+    const int cv = p.cv = bulk ? (p.C + 7) / 8 : (p.C + 14) / 8;
     p.nb_log2 = p.K <= 256 ? 2 : 1;
     for (p.cl = 1; p.cl <= 8; p.cl *= 2) {
         p.vp = (cv + p.cl - 1) / p.cl;
@@ -934,7 +946,7 @@ cudaError_t launch_distill(DistillArgs p, cudaStream_t st)
         p.nw = (p.vp + p.wv - 1) / p.wv;
         for (p.ns = 3; p.ns >= 2; p.ns--) {
             const uint32_t smem = layout_of(p.nw, p.ns, p.per, p.cl, p.K, 1 << p.nb_log2).total;
-            if (smem <= kSmemLimit) return bulk ? launch_rounds<true>(rounds, p, smem, st) : launch_rounds<false>(rounds, p, smem, st);
+            if (smem <= kSmemLimit) return bulk ? launch_rounds<false>(rounds, p, smem, st) : launch_rounds<true>(rounds, p, smem, st);
         }
     }
     p.cl = 4;
@@ -948,7 +960,7 @@ cudaError_t launch_distill(DistillArgs p, cudaStream_t st)
         if (smem <= kSmemLimit) break;
     }
     if (p.per < 64) return cudaErrorInvalidConfiguration;
-    return bulk ? run(k_distill_stream<true>, 2 * kMaxRounds, 0, p, smem, st) : run(k_distill_stream<false>, 2 * kMaxRounds + 1, 0, p, smem, st);
+    return bulk ? run(k_distill_stream<false>, 2 * kMaxRounds, 0, p, smem, st) : run(k_distill_stream<true>, 2 * kMaxRounds + 1, 0, p, smem, st);
 }
 
 }  // namespace

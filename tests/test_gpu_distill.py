@@ -91,7 +91,8 @@ SHAPES = [  # B, C, K, pitch, shift
     (33, 1003, 5, 1003, 0), (40, 8000, 64, 8000, 3), (700, 257, 100, 264, 0), (500, 32000, 64, 32000, 0), (310, 20011, 20, 20016, 0),
     (3, 32000, 16, 32000, 0), (80, 36001, 16, 36008, 0), (160, 60000, 16, 60000, 0), (40, 100001, 1000, 100008, 0), (20, 200001, 7, 200008, 0),
     (9, 420000, 12, 420000, 0), (33, 300007, 300, 300008, 0), (20, 1000003, 50, 1000008, 0), (40, 830000, 20, 830000, 0), (40, 500009, 40, 500016, 0), (2, 793471, 128, 793472, 0), (25, 600000, 5, 600000, 1), (30, 700, 1024, 704, 0),
-    (6, 400001, 1024, 400008, 0), (70, 262144, 33, 262144, 0), (160, 16384, 64, 16384, 0), (1000, 2048, 40, 2048, 0)]
+    (6, 400001, 1024, 400008, 0), (70, 262144, 33, 262144, 0), (3, 1, 1, 1, 5), (9, 5, 4, 5, 1), (7, 6, 3, 6, 7), (20, 13, 5, 14, 2), (300, 32001, 64, 32001, 3),
+    (12, 100001, 20, 100001, 6), (5, 793471, 30, 793471, 0), (20, 50257, 9, 50259, 1), (160, 16384, 64, 16384, 0), (1000, 2048, 40, 2048, 0)]
 
 
 @pytest.mark.parametrize("B,C,K,ld,shift", SHAPES)
@@ -104,6 +105,27 @@ def test_loss_and_gradient(B, C, K, ld, shift):
     assert torch.equal(got[0], again[0]) and torch.equal(got[1], again[1])
     only = call(z, t, idx, tau, S, ld, shift, K + 3, want_dz=False)
     assert torch.equal(only[1], got[1])
+
+
+@pytest.mark.parametrize("C,ldz,lddz,shift", [(1003, 1008, 1003, 0), (1003, 1003, 1008, 0), (32001, 32001, 32001, 1), (5, 5, 6, 3), (800001, 800001, 800008, 0)])
+def test_gradient_rows_that_lie_otherwise_than_the_logits(C, ldz, lddz, shift):
+    from paper_1710_03740_b200 import binding as b
+    B, K, tau, S = 9, 5, 2.0, 64.0
+    z, t, idx = make(B, C, K, C + shift)
+    idx[4] = -1
+    ref = call(z, t, idx, tau, S)
+    check(z, t, idx, tau, S, ref)
+    zd = torch.full((B, ldz), float("nan"), dtype=torch.float16, device="cuda")
+    zd[:, :C] = torch.from_numpy(z)
+    buf = torch.full((B * lddz + shift + 8,), 7.0, dtype=torch.float16, device="cuda")
+    dz = buf[shift:shift + B * lddz].view(B, lddz)
+    rl, loss = torch.empty(B, device="cuda"), torch.empty(1, device="cuda")
+    b.mpt_distill_topk(zd, ldz, B, C, torch.from_numpy(t).cuda(), torch.from_numpy(idx).cuda(), K, K, tau, S, dz, lddz, rl, loss)
+    torch.cuda.synchronize()
+    check(z, t, idx, tau, S, (dz[:, :C].double(), rl.double(), float(loss)))
+    outside = torch.ones_like(buf, dtype=torch.bool)
+    outside[shift:shift + B * lddz].view(B, lddz)[:, :C] = False
+    assert bool((buf[outside] == 7.0).all())
 
 
 @pytest.mark.parametrize("C,ld", [(50, 50), (1000, 1000), (32000, 32000), (100000, 100000), (500000, 500000)])
