@@ -517,8 +517,8 @@ void mpt_lstm_destroy(mpt_lstm_ctx *ctx);
  * (results are then invalid).
  * workspace: mpt_layernorm_workspace_bytes, 16-byte aligned, owned by the caller and in use until the call's
  * stream work has completed (calls that may overlap need one each).  Results are run-to-run identical.
- * Rows that are 16-byte aligned (base pointers, and pitches that are multiples of 8) move by bulk copies and 16-byte
- * stores, others element by element; rows of more than 16384 features forward, 12288 backward, are read more than once (by kernels
+ * Fastest where all rows and the parameters are 16-byte aligned (base pointers, and pitches that are multiples of 8); rows
+ * that are not are shifted on the way (about 1.6 times as long); rows of more than 16384 features forward, 12288 backward, are read more than once (by kernels
  * that keep nothing of a row on chip).  cols from 1 to 2^30, rows from 0 to 2^30 (MPT_ERR_SHAPE otherwise).  Outputs must not overlap inputs (the same pointer is
  * refused).  rows == 0: forward does nothing, backward writes zero dgamma and dbeta.  The stream must belong to
  * the current device (the launch fails otherwise: MPT_ERR_CUDA).  Bytes moved per element: 4 forward, 6 backward. */

@@ -17,8 +17,10 @@
 // The backward pass adds dy*h and dy into per-lane FP32 column sums, leaves one partial row of them per CTA in the
 // workspace and adds those in a second kernel in a fixed order: results are run-to-run identical, nothing is added
 // atomically.  The partial sums are at most 148 rows whatever the batch.
-// Measured: 4096 x 12288 forward 45 us (4.5 TB/s), 40960 x 1024 forward 33 (5.1 TB/s), backward 52 us (4.8 TB/s), 2047 x 8191
-// backward 32 us.  Rows that are not 16-byte aligned: 4096 x 12287 199 and 440 us.
+// Rows that lie across 16-byte boundaries are copied in the vectors that they lie in, shifted as a lane takes them, and
+// shifted back between lanes on the way out.
+// Measured: 4096 x 12288 forward 44 us (4.6 TB/s), 40960 x 1024 forward 33 (5.1 TB/s), backward 52 us (4.8 TB/s), 2047 x 8191
+// backward 32 us; 4096 x 12287 without a pitch 69 and 148 us.
 #include <math.h>
 
 #include "mpt_common.cuh"
@@ -172,9 +174,12 @@ constexpr int kLnFwdWarps = 24;       // warps of a CTA of the forward kernel
 constexpr __host__ __device__ int ln_bwd_warps(int R) { return R <= 2 ? 16 : 12; }
 // Buffers of a warp: as many as shared memory has room for beside the scale and shift vectors.
 constexpr __host__ __device__ int ln_buffers(int inputs) { return inputs == 1 ? 3 : 4; }
-// Shared memory of a CTA: buffers [warps][ln_buffers][inputs][32 R] of 16 bytes | the scale vector (forward: and the shift vector)
+// Shared memory of a CTA: buffers [warps][ln_buffers][inputs][32 R + 1] of 16 bytes | the scale vector (forward: and the shift vector)
 // [row_warps][32 R] | mbarriers [warps][ln_buffers].
-constexpr __host__ __device__ uint32_t ln_params_at(int warps, int R, int inputs) { return (uint32_t)(warps * ln_buffers(inputs) * inputs * R * 512); }
+constexpr __host__ __device__ uint32_t ln_params_at(int warps, int R, int inputs) 
+{
+    return (uint32_t)(warps * ln_buffers(inputs) * inputs * (R * 512 + 16));
+}
 constexpr __host__ __device__ uint32_t ln_bars_at(int warps, int row_warps, int R, int inputs)
 {
     return ln_params_at(warps, R, inputs) + (uint32_t)((inputs == 1 ? 2 : 1) * row_warps * R * 512);
@@ -197,7 +202,8 @@ struct LnWarp {
     uint32_t *status;
     bool dead = false;
 
-    static constexpr int kSlot = NIN * R * 32;      // vectors of a buffer
+    static constexpr int kPart = R * 32 + 1;        // vectors of an input in a buffer: a part that lies across 16-byte boundaries touches one more
+    static constexpr int kSlot = NIN * kPart;
     static constexpr int kBuffers = ln_buffers(NIN);
 
     __device__ __forceinline__ LnWarp(uint8_t *smem, int row_warps, int rows_, int cols_, volatile uint32_t *abort, uint32_t *status_)
@@ -228,33 +234,70 @@ struct LnWarp {
         __syncthreads();
     }
     __device__ __forceinline__ int row_of(int i) const { return first + i * stride; }
-    // Row i into the next buffer (which is free).  A last, partial vector comes whole with what the pitch leaves behind it
-    // (take() clears that), but for the matrix's last row, whose memory may end with it: there element by element.
+    // Elements between the 16-byte boundary before row i of a matrix and its start (BULK: none).
+    __device__ __forceinline__ int shift(const uint16_t *base, size_t pitch, int i) const
+    {
+        return BULK ? 0 : (int)((((uintptr_t)base >> 1) + (size_t)row_of(i) * pitch) & 7);
+    }
+    // Row i into the next buffer (which is free), in the vectors that it lies in.  Vectors that it shares come whole (take()
+    // clears what lies behind the row), but for one that reaches out of the matrix's memory: by elements.
     __device__ __forceinline__ void request(int i)
     {
         if (i >= n) return;
         uint4 *dst = buf + s_ask * kSlot;
-        const int whole = row_of(i) == rows - 1 ? min(nv, cols / 8 - v0) : nv;
+        const int row = row_of(i), length = min(nv * 8, cols - v0 * 8);       // elements of this warp's part
         const uint32_t b = bar + 8u * (uint32_t)s_ask;
-        if (BULK && lane == 0) {
-            if (whole > 0) mbar_arrive_expect_tx(b, (uint32_t)(NIN * whole) * 16u);
-            else mbar_arrive(b);
-        }
+        const uint16_t *from[NIN];
+        int lo[NIN], hi[NIN], bytes = 0;
 #pragma unroll
         for (int k = 0; k < NIN; k++) {
-            const uint16_t *from = src[k] + (size_t)row_of(i) * ld[k] + (size_t)v0 * 8;
-            uint4 *to = dst + k * R * 32;
-            if (BULK) {
-                if (lane == 0 && whole > 0)
-                    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                                 ::"r"(smem_u32(to)), "l"(from), "r"((uint32_t)whole * 16u), "r"(b) : "memory");
-                if (whole < nv && lane < 8) ((uint16_t *)(to + whole))[lane] = (v0 + whole) * 8 + lane < cols ? from[whole * 8 + lane] : (uint16_t)0;
-            } else {
-                for (int e = lane; e < nv * 8; e += 32) ((uint16_t *)to)[e] = v0 * 8 + e < cols ? from[e] : (uint16_t)0;
+            const int sh = shift(src[k], ld[k], i);
+            const size_t at = (size_t)row * ld[k] + (size_t)v0 * 8;
+            from[k] = src[k] + ((ptrdiff_t)at - sh);
+            lo[k] = !BULK && at < (size_t)sh ? 1 : 0;
+            const int touched = (sh + length + 7) / 8;
+            hi[k] = touched - (at - sh + (size_t)touched * 8 > (size_t)(rows - 1) * ld[k] + (size_t)cols ? 1 : 0);
+            if (hi[k] < lo[k]) hi[k] = lo[k];
+            bytes += (hi[k] - lo[k]) * 16;
+            if (lane < 8 && (lo[k] > 0 || hi[k] < touched)) {
+                uint16_t *to = (uint16_t *)(dst + k * kPart);
+                auto elements = [&](int v) {
+                    const int e = v * 8 + lane;
+                    to[e] = e >= sh && e < sh + length ? from[k][e] : (uint16_t)0;
+                };
+                if (lo[k] > 0) elements(0);
+                if (hi[k] < touched) elements(touched - 1);
             }
         }
         __syncwarp();
+        if (lane == 0) {
+            if (bytes > 0) mbar_arrive_expect_tx(b, (uint32_t)bytes);
+            else mbar_arrive(b);
+#pragma unroll
+            for (int k = 0; k < NIN; k++)
+                if (hi[k] > lo[k])
+                    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                                 ::"r"(smem_u32(dst + k * kPart + lo[k])), "l"(from[k] + lo[k] * 8), "r"((uint32_t)(hi[k] - lo[k]) * 16u), "r"(b)
+                                 : "memory");
+        }
+        __syncwarp();
         s_ask = s_ask + 1 == kBuffers ? 0 : s_ask + 1;
+    }
+    // Eight neighbouring elements from the `from`-th of the sixteen of two vectors on.
+    __device__ __forceinline__ static uint4 across(const uint4 a, const uint4 b, int from)
+    {
+        uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        if (from & 4) {
+#pragma unroll
+            for (int i = 0; i < 6; i++) w[i] = w[i + 2];
+        }
+        if (from & 2) {
+#pragma unroll
+            for (int i = 0; i < 5; i++) w[i] = w[i + 1];
+        }
+        const uint32_t s = (uint32_t)(from & 1) * 16u;
+        return make_uint4(__funnelshift_r(w[0], w[1], s), __funnelshift_r(w[1], w[2], s), __funnelshift_r(w[2], w[3], s),
+                          __funnelshift_r(w[3], w[4], s));
     }
     // Keeps the first `left` of eight values, zeros behind them.
     __device__ __forceinline__ static void clear_behind(uint4 &v, int left)
@@ -264,11 +307,11 @@ struct LnWarp {
         v.z = left >= 6 ? v.z : (left == 5 ? v.z & 0xFFFFu : 0u);
         v.w = left >= 8 ? v.w : (left == 7 ? v.w & 0xFFFFu : 0u);
     }
-    // The next row into registers (zeros from the last feature on).
+    // Row i, the next one, into registers (zeros from the last feature on).
     template <bool WHOLE>
-    __device__ __forceinline__ void take(uint4 (&x)[NIN][R])
+    __device__ __forceinline__ void take(int i, uint4 (&x)[NIN][R])
     {
-        if (BULK && !mbar_try_wait(bar + 8u * (uint32_t)s_use, parity) && !mbar_wait(bar + 8u * (uint32_t)s_use, parity, abort_flag)) {
+        if (!mbar_try_wait(bar + 8u * (uint32_t)s_use, parity) && !mbar_wait(bar + 8u * (uint32_t)s_use, parity, abort_flag)) {
             // all later waits of the CTA end at once; what is computed from here on is not valid
             if (status && !*abort_flag) atomicCAS(status, 0u, (uint32_t)KERR_WAIT_FULL | 0x40u | ((uint32_t)blockIdx.x << 8));
             *abort_flag = 1u;
@@ -277,10 +320,12 @@ struct LnWarp {
         const uint4 *from = buf + s_use * kSlot;
 #pragma unroll
         for (int k = 0; k < NIN; k++) {
+            const int sh = shift(src[k], ld[k], i);
 #pragma unroll
             for (int u = 0; u < R; u++) {
                 const int j = lane + 32 * u;
-                x[k][u] = WHOLE || j < nv ? from[k * R * 32 + j] : make_uint4(0u, 0u, 0u, 0u);
+                x[k][u] = WHOLE || j < nv ? from[k * kPart + j] : make_uint4(0u, 0u, 0u, 0u);
+                if (!BULK && sh > 0) x[k][u] = across(x[k][u], WHOLE || j < nv ? from[k * kPart + j + 1] : x[k][u], sh);
                 if (!WHOLE && !whole(u)) clear_behind(x[k][u], cols - (v0 + j) * 8);
             }
         }
@@ -315,7 +360,40 @@ struct LnWarp {
         __syncthreads();
     }
     // whether the warp's vectors 32 u ... 32 u + 31 are all whole (the same for all lanes)
-    __device__ __forceinline__ bool whole(int u) const { return BULK && (v0 + 32 * (u + 1)) * 8 <= cols; }
+    __device__ __forceinline__ bool whole(int u) const { return (v0 + 32 * (u + 1)) * 8 <= cols; }
+    // The warp's part of row i of a result, by 16-byte stores: the vectors between 16-byte boundaries of the output are put
+    // together from a lane's own and its neighbour's elements; at the ends of the part, element by element.
+    __device__ __forceinline__ void put(uint16_t *base, size_t pitch, int i, const uint4 (&y)[R]) const
+    {
+        uint16_t *o = base + (size_t)row_of(i) * pitch;
+        const int sh = shift(base, pitch, i);
+        uint4 before = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int u = 0; u < R; u++) {
+            const int j = lane + 32 * u, at = (v0 + j) * 8;
+            if (BULK || sh == 0) {
+                if (j < nv) store8<true>(o, at, cols, y[u]);
+                continue;
+            }
+            const int left = (lane + 31) & 31;
+            const uint4 turned = make_uint4(__shfl_sync(0xFFFFFFFFu, y[u].x, left), __shfl_sync(0xFFFFFFFFu, y[u].y, left),
+                                            __shfl_sync(0xFFFFFFFFu, y[u].z, left), __shfl_sync(0xFFFFFFFFu, y[u].w, left));
+            const uint4 v = across(lane == 0 ? before : turned, y[u], 8 - sh);
+            before = turned;
+            if (j >= nv) continue;
+            if (j > 0 && at - sh + 8 <= cols) __stcs((uint4 *)(o + (at - sh)), v);
+            else elements(o, at - sh, v, j > 0 ? at - sh : at, cols);
+            if (j == nv - 1) elements(o, at, y[u], at - sh + 8, cols);
+        }
+    }
+    // Those of eight elements from `at` on that lie in [lo, hi).
+    __device__ __forceinline__ static void elements(uint16_t *o, int at, const uint4 v, int lo, int hi)
+    {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 8; e++)
+            if (at + e >= lo && at + e < hi) o[at + e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+    }
 };
 
 // A scale or shift vector (null: zeros) to shared memory, zeros from the last feature on; all loads are asked for before the
@@ -376,7 +454,7 @@ __global__ void __launch_bounds__(kLnFwdWarps * 32, 1) k_ln_fwd(const LnFwd p)
         constexpr bool W = decltype(whole)::value;
         for (int i = 0; i < c.n; i++) {
             uint4 x[1][R];
-            c.template take<W>(x);
+            c.template take<W>(i, x);
             c.request(i + c.kBuffers);
             f2 f[R][4];
             f2 s = pair(0.0f, 0.0f);
@@ -413,22 +491,19 @@ __global__ void __launch_bounds__(kLnFwdWarps * 32, 1) k_ln_fwd(const LnFwd p)
                 if (p.mean) p.mean[row] = mean;
                 if (p.rstd) p.rstd[row] = rstd;
             }
-            uint16_t *yr = p.y + (size_t)row * p.ldy + col0;
             const f2 r2 = pair(rstd, rstd);
+            uint4 y[R];
 #pragma unroll
             for (int u = 0; u < R; u++) {
-                const int col = col0 + 256 * u;
-                const bool whole_u = W || c.whole(u);
-                if (whole_u || col < p.cols) {
-                    f2 g[4], b[4];
-                    widen8(gamma[32 * u], g);
-                    widen8(beta[32 * u], b);
+                f2 g[4], b[4];
+                widen8(gamma[32 * u], g);
+                widen8(beta[32 * u], b);
 #pragma unroll
-                    for (int e = 0; e < 4; e++) f[u][e] = fma2(mul2(f[u][e], r2), g[e], b[e]);
-                    if (whole_u) __stcs((uint4 *)(yr + 256 * u), round8(f[u]));
-                    else store8<BULK>(yr - col0, col, p.cols, round8(f[u]));
-                }
+                for (int e = 0; e < 4; e++) f[u][e] = fma2(mul2(f[u][e], r2), g[e], b[e]);
+                y[u] = round8(f[u]);
+                if (BULK && W) __stcs((uint4 *)(p.y + (size_t)row * p.ldy + col0 + 256 * u), y[u]);
             }
+            if (!(BULK && W)) c.put(p.y, p.ldy, i, y);
         }
     };
     if (c.whole(R - 1)) rows(Whole{});
@@ -545,7 +620,7 @@ __global__ void __launch_bounds__(ln_bwd_warps(R) * 32, 1) k_ln_bwd(const LnBwd 
             const float mean = __shfl_sync(0xFFFFFFFFu, mean32, i & 31), rstd = __shfl_sync(0xFFFFFFFFu, rstd32, i & 31);
             const f2 minus = pair(-mean, -mean), r2 = pair(rstd, rstd);
             uint4 v[2][R];
-            c.template take<W>(v);
+            c.template take<W>(i, v);
             c.request(i + c.kBuffers);
             f2 h[R][4], gy[R][4];
             f2 s1 = pair(0.0f, 0.0f), s2 = s1;
@@ -583,17 +658,15 @@ __global__ void __launch_bounds__(ln_bwd_warps(R) * 32, 1) k_ln_bwd(const LnBwd 
             }
             const float m1 = -rstd * (c1 * inv_n), m2 = -rstd * (c2 * inv_n);
             const f2 k1 = pair(m1, m1), k2 = pair(m2, m2);
-            uint16_t *o = p.dx + (size_t)c.row_of(i) * p.lddx + col0;
+            uint4 o[R];
 #pragma unroll
             for (int u = 0; u < R; u++) {
-                const bool whole_u = W || c.whole(u);
-                if (whole_u || col0 + 256 * u < p.cols) {
 #pragma unroll
-                    for (int e = 0; e < 4; e++) gy[u][e] = fma2(gy[u][e], r2, fma2(h[u][e], k2, k1));
-                    if (whole_u) __stcs((uint4 *)(o + 256 * u), round8(gy[u]));
-                    else store8<BULK>(o - col0, col0 + 256 * u, p.cols, round8(gy[u]));
-                }
+                for (int e = 0; e < 4; e++) gy[u][e] = fma2(gy[u][e], r2, fma2(h[u][e], k2, k1));
+                o[u] = round8(gy[u]);
+                if (BULK && W) __stcs((uint4 *)(p.dx + (size_t)c.row_of(i) * p.lddx + col0 + 256 * u), o[u]);
             }
+            if (!(BULK && W)) c.put(p.dx, p.lddx, i, o);
         }
     };
     if (c.whole(R - 1)) rows(Whole{});

@@ -111,7 +111,39 @@ def ref_backward(dy, x, gamma, mean, rstd):
 SHAPES = [(1, 1, 1, 0), (1, 8, 8, 0), (3, 7, 7, 0), (5, 64, 64, 0), (64, 256, 256, 0), (33, 255, 256, 0), (9, 300, 301, 0),
           (150, 1000, 1000, 0), (17, 1024, 1032, 0), (1200, 1024, 1024, 0), (21, 1025, 1032, 0), (40, 2048, 2048, 0),
           (300, 4095, 4096, 0), (31, 6144, 6144, 0), (7, 6145, 6152, 0), (149, 12288, 12288, 0), (5, 12287, 12288, 0),
-          (12, 1024, 1024, 3), (6, 5000, 5001, 1), (3, 12296, 12296, 0), (300, 768, 768, 0), (160, 16384, 16384, 0), (33, 15001, 15008, 0), (3, 16392, 16392, 0), (600, 8184, 8192, 0), (2, 33000, 33000, 0), (5, 40001, 40001, 1)]
+          (12, 1024, 1024, 3), (6, 5000, 5001, 1), (3, 12296, 12296, 0), (300, 768, 768, 0), (160, 16384, 16384, 0), (33, 15001, 15008, 0), (3, 16392, 16392, 0), (600, 8184, 8192, 0), (5, 8191, 8191, 0), (300, 2047, 2047, 0), (150, 255, 255, 1),
+          (17, 12287, 12287, 5), (4, 1, 1, 3), (6, 9, 9, 1), (5, 5, 6, 7), (600, 1001, 1003, 2), (40, 16383, 16383, 0), (2, 33000, 33000, 0), (5, 40001, 40001, 1)]
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 3), (7, 30), (310, 1000), (9, 4099), (33, 9001)])
+def test_matrices_that_lie_differently_to_16_byte_boundaries(rows, cols):
+    from paper_1710_03740_b200 import binding as b
+    x, dy, gamma, beta = make(rows, cols, rows + cols)
+    (xd, _), (dyd, _) = pitched(x, cols + 3, 5, fill=float("nan")), pitched(dy, cols + 1, 2, fill=float("nan"))
+    (yd, ybuf), (dxd, dxbuf) = pitched(np.full_like(x, 7.0), cols + 6, 1, fill=7.0), pitched(np.full_like(x, 7.0), cols + 9, 4, fill=7.0)
+    gbuf = torch.zeros(cols + 3, dtype=torch.float16, device="cuda")
+    gd = gbuf[3:]
+    gd.copy_(torch.from_numpy(gamma))
+    bd = torch.from_numpy(beta).cuda()
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    dg, db = torch.empty(cols, dtype=torch.float16, device="cuda"), torch.empty(cols, dtype=torch.float16, device="cuda")
+    ws = torch.empty(b.mpt_layernorm_workspace_bytes(rows, cols), dtype=torch.uint8, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    b.mpt_layernorm_forward(rows, cols, xd, cols + 3, gd, bd, 1e-5, yd, cols + 6, mean, rstd, status)
+    b.mpt_layernorm_backward(rows, cols, dyd, cols + 1, xd, cols + 3, gd, mean, rstd, dxd, cols + 9, dg, db, ws, status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    ry, _, _, tol = ref_forward(x, gamma, beta, 1e-5)
+    assert np.all(np.abs(yd.cpu().numpy() - ry) <= tol)
+    # the aligned call's results, to the bit: the same sums in the same order
+    wy, wmean, wrstd = forward(x, gamma, beta, 1e-5, (cols + 7) // 8 * 8)
+    assert np.array_equal(wy, yd.cpu().numpy()) and np.array_equal(wmean, mean.cpu().numpy()) and np.array_equal(wrstd, rstd.cpu().numpy())
+    wdx, wdg, wdb, _ = backward(dy, x, gamma, wmean, wrstd, (cols + 7) // 8 * 8)
+    assert np.array_equal(wdx, dxd.cpu().numpy()) and np.array_equal(wdg, dg.cpu().numpy()) and np.array_equal(wdb, db.cpu().numpy())
+    for buf, ld, shift in ((ybuf, cols + 6, 1), (dxbuf, cols + 9, 4)):
+        outside = torch.ones_like(buf, dtype=torch.bool)
+        outside[shift:shift + rows * ld].view(rows, ld)[:, :cols] = False
+        assert bool((buf[outside] == 7.0).all())
 
 
 @pytest.mark.parametrize("rows,cols,ld,shift", SHAPES)
