@@ -4,17 +4,18 @@
 //   q = softmax over the row's entries of t / tau ;  p = softmax over all C classes of z / tau
 //   loss = tau^2 sum_j q_j (log q_j - log p_c(j)) ;  dz_v = rn16(tau * (p_v - sum of q_j with c(j) = v) * S / B)
 //
-// Bound: HBM, 4 bytes a logit (z read once, dz written once).  A row is spread over up to 16 warps of a CTA or over a
-// cluster of 2, 4 or 8 CTAs.  Each warp sums the exponentials of its part of a row and turns them into the gradient.
-// What warps exchange is one (reference, sum) pair per row, through (distributed) shared memory and an mbarrier; two
-// more warps per CTA prepare the teacher's entries rows ahead.
-//   Up to 32768 logits per CTA (262144 per row) a further warp moves whole rows in and out by bulk copies, and the
-// exponentials stay in registers between the two uses, each lane's relative to its own maximum: one special-function
-// result and about 6 instructions a logit (4096 x 32000 109 us = 4.8 TB/s, 2001 x 20011 43 us, 4096 x 32001 without a pitch,
-// where every row lies differently to 16-byte boundaries, 119 us).
-//   Longer rows pass through shared memory twice, the second time from L2 (clusters of 4: about 33 rows of 1.6 MB are
-// in work at a time; first reads are marked to stay, second reads and the gradient to leave first), and take their
-// exponentials twice (512 x 793471 416 us).
+// Bound: HBM, 4 bytes a logit (z read once, dz written once).  Three kernels, by the length of a row:
+//   up to 2048 classes (and 256 entries): k_distill_rows, a warp a row.
+//   up to 32768: k_distill, a row spread over up to 16 warps of a CTA.  Each warp sums the exponentials of its part and turns
+// them into the gradient; what warps exchange is one (reference, sum) pair per row, through shared memory and an mbarrier; two
+// more warps prepare the teacher's entries rows ahead, a further one moves whole rows in and out by bulk copies.  The
+// exponentials stay in registers between the two uses, each lane's relative to its own maximum: one special-function result
+// and about 6 instructions a logit (4096 x 32000 102 us = 5.1 TB/s, 2001 x 20011 43 us, 4096 x 32001 without a pitch, where
+// every row lies differently to 16-byte boundaries, 117 us).
+//   longer: k_distill_stream.  A row passes through shared memory twice, the second time from L2 (first reads are marked to
+// stay, second reads and the gradient to leave first), and its exponentials are taken twice (512 x 793471 364 us); where there
+// are few rows, or where that evens out the last round, the CTAs of a cluster share it and exchange the pairs through
+// distributed shared memory.
 #include <math.h>
 
 #include "mpt_common.cuh"
@@ -46,6 +47,7 @@ struct DistillArgs {
     int ns;              // buffers per warp
     int nb_log2;         // buffers for a row's entries: 2^nb_log2
     int per;             // vectors per buffer: wv, or a chunk of it where rows are streamed
+    int kept;            // the teacher's classes' logits are kept with the entries (else the row's loss reads them again)
     int same;            // rows of dz lie to 16-byte boundaries as those of z do
 };
 
@@ -73,7 +75,8 @@ constexpr int kTeachers = 2;         // warps that prepare the teacher's entries
 constexpr unsigned kNap = 64;        // ns
 constexpr int kAhead = 4;            // rows of its own a teacher warp asks for ahead
 constexpr int kMaxWarps = 16;        // warps that hold logits: few, so that what each does once per row stays small
-constexpr int kMaxRounds = 8;        // vectors a lane keeps in registers
+constexpr int kMinRounds = 4, kMaxRounds = 8;      // vectors a lane keeps in registers
+constexpr int kHalfWarps = 8;        // CTAs of so many warps with logits are compiled to fit twice on an SM
 constexpr int kChunk = 256;          // vectors of a buffer where rows are streamed
 constexpr int kMaxBatch = 1 << 30;   // what is added to row indexes stays inside 32 bits
 constexpr uint32_t kNegInf16 = 0xFC00u;
@@ -237,11 +240,28 @@ __device__ __forceinline__ void patch_targets(uint16_t *dst, int first, int coun
     }
 }
 
+// The first entries of a row's list, asked for ahead of their use.
+struct ListAhead {
+    static constexpr int N = 4;          // a lane
+    int v[N];
+    uint16_t t[N];
+    __device__ __forceinline__ void ask(const DistillArgs &p, int row)
+    {
+        const size_t at = (size_t)row * p.ldt;
+#pragma unroll
+        for (int c = 0; c < N; c++) {
+            const int j = (int)(threadIdx.x & 31) + 32 * c;
+            v[c] = j < p.K ? p.idx[at + j] : kNoClass;
+            t[c] = j < p.K ? p.t[at + j] : (uint16_t)kNegInf16;
+        }
+    }
+};
 // Teacher's entries of a row, by one warp.  Entries whose class is outside [0, C) or whose logit is -inf have no part;
 // returns whether any has.  `rank`: which CTA of the cluster this is.
 // Classes named more than once are found with a hash table (open addressing, `slots` words, a
 // power of two and at least 2 K); only theirs are added up, over the entries in order.
-__device__ __forceinline__ bool prepare_entries(const DistillArgs &p, int row, int rank, int shift, const Entries &ent, int *table, int slots)
+__device__ __forceinline__ bool prepare_entries(const DistillArgs &p, int row, int rank, int shift, const ListAhead &ahead, const Entries &ent, int *table,
+                                                int slots)
 {
     const int lane = threadIdx.x & 31;
     const int32_t *id = p.idx + (size_t)row * p.ldt;
@@ -251,16 +271,19 @@ __device__ __forceinline__ bool prepare_entries(const DistillArgs &p, int row, i
     float top = -INFINITY;
     bool any = false;
     __syncwarp();
-#pragma unroll 4
-    for (int j = lane; j < p.K; j += 32) {
-        const int v = id[j];
-        const float t = h2f(tt[j]);
+    auto enter = [&](int j, int v, uint16_t t16) {
+        const float t = h2f(t16);
         const bool ok = v >= 0 && v < p.C && t != -INFINITY;
         ent.v[j] = ok ? v : kNoClass;
         ent.q[j] = t;
         if (ok) top = fmaxf(top, t);
         any |= ok;
-    }
+    };
+#pragma unroll
+    for (int c = 0; c < ListAhead::N; c++)
+        if (lane + 32 * c < p.K) enter(lane + 32 * c, ahead.v[c], ahead.t[c]);
+#pragma unroll 4
+    for (int j = lane + 32 * ListAhead::N; j < p.K; j += 32) enter(j, id[j], tt[j]);
     top = wmax(top);
     float s = 0.0f;
     bool twice = false;
@@ -334,8 +357,7 @@ __device__ __forceinline__ void write_loss(const DistillArgs &p, int row, const 
         const int v = ent.v[j];
         // log2 q - log2 p; a probability of zero (or none) adds nothing
         if (v >= 0 && !(q == 0.0f)) {
-            // a CTA that holds the whole row has kept the logits; in a cluster they are read again
-            const float z = p.cl == 1 ? ent.z[j] : h2f(zr[v]);
+            const float z = p.kept ? ent.z[j] : h2f(zr[v]);
             l += q * ((log2f(q) + l2s) - fmaf(z, p.k, -pr.x));
         }
     }
@@ -432,7 +454,7 @@ struct Cta {
     {
         warp = threadIdx.x >> 5;
         lane = threadIdx.x & 31;
-        rank = p.cl > 1 ? (int)cluster_ctarank() : 0;
+        rank = !ROWS && p.cl > 1 ? (int)cluster_ctarank() : 0;      // ROWS: no clusters
         cluster = (int)blockIdx.x / p.cl;
         clusters = (int)gridDim.x / p.cl;
         n_rows = cluster < p.B ? (p.B - 1 - cluster) / clusters + 1 : 0;
@@ -615,7 +637,7 @@ struct Cta {
     __device__ __forceinline__ void publish(int i, float2 pr)
     {
         float2 *slot = red(i) + rank * p.nw + warp;
-        if (p.cl == 1) {
+        if (ROWS || p.cl == 1) {
             if (lane == 0) {
                 *slot = pr;
                 mbar_arrive(pair_bar(i));
@@ -631,7 +653,7 @@ struct Cta {
     __device__ __forceinline__ float2 collect(int i)
     {
         const uint32_t parity = (uint32_t)(i / kPairBuffers) & 1u;
-        if (p.cl == 1) wait<false>(pair_bar(i), parity);
+        if (ROWS || p.cl == 1) wait<false>(pair_bar(i), parity);
         else wait<true>(pair_bar(i), parity);
         return row_pair(red(i), pairs);
     }
@@ -664,6 +686,9 @@ struct Cta {
     __device__ __forceinline__ void teach()
     {
         const int me = warp - p.nw, nb = 1 << p.nb_log2;
+        ListAhead ahead;
+        if (me < n_rows) ahead.ask(p, row_of(me));
+        for (int r = 1; r < kAhead; r++) prefetch_list(me + r * kTeachers);
         for (int i = me; i < n_rows + nb; i += kTeachers) {
             const int b = i & (nb - 1);
             const uint32_t parity = ((uint32_t)(i >> p.nb_log2) & 1u) ^ 1u;
@@ -673,14 +698,13 @@ struct Cta {
             if (i >= nb && rank == 0 && !dead) write_loss(p, row_of(i - nb), entries(b), *live(b) != 0, *pair_of(b));
             if (i < n_rows) {
                 __syncwarp();
-                if (i == me)
-                    for (int r = 1; r < kAhead; r++) prefetch_list(i + r * kTeachers);
                 prefetch_list(i + kAhead * kTeachers);
-                const bool any = prepare_entries(p, row_of(i), rank, shift(i), entries(b), (int *)(smem + L.table) + me * L.slots, L.slots);
+                const bool any = prepare_entries(p, row_of(i), rank, shift(i), ahead, entries(b), (int *)(smem + L.table) + me * L.slots, L.slots);
                 if (lane == 0) {
                     *live(b) = any ? 1 : 0;
                     mbar_arrive(full_bar(b));
                 }
+                if (i + kTeachers < n_rows) ahead.ask(p, row_of(i + kTeachers));      // arrives while this warp waits
             }
         }
     }
@@ -701,8 +725,10 @@ struct Cta {
 };
 
 // Rows whose exponentials stay in registers: R vectors per lane.
-template <int R, bool SHIFT>
-__global__ void __launch_bounds__((kMaxWarps + kTeachers + 1) * 32, 1) k_distill(const DistillArgs p)
+// HALF: for CTAs of at most kHalfWarps (+ 3) warps, with the registers that let two of them reside on an SM; the rows of the
+// two hide each other's waits (5000 x 8000 79 -> 52 us; with 16 warps the fewer registers cost more: 5000 x 16000 92 -> 112).
+template <int R, bool SHIFT, bool HALF>
+__global__ void __launch_bounds__((HALF ? 2 * (kHalfWarps + kTeachers + 1) : kMaxWarps + kTeachers + 1) * 32, 1) k_distill(const DistillArgs p)
 {
     pdl_trigger();
     extern __shared__ __align__(128) uint8_t smem[];
@@ -864,23 +890,200 @@ __global__ void __launch_bounds__((kMaxWarps + kTeachers) * 32, 1) k_distill_str
     c.leave();
 }
 
+// Short rows: a warp for each, which also prepares the teacher's entries; nothing is exchanged and the warps of an SM hide each
+// other's waits (4096 x 1000 with 8 entries takes 24 us by the kernel above, whose rows pass through four warps of a CTA one
+// after the other).  MEAN: the grid is one cluster, which also takes the mean of the losses.
+constexpr int kRowWarps = 8;
+constexpr int kRowMaxK = 256;         // entries: what shared memory holds for kRowWarps rows
+constexpr int kMeanRows = 64;         // rows of a call that one cluster works on, a row a warp (200 rows: 16 us, with two launches 13)
+struct RowLayout {
+    uint32_t ent, table, total;       // of a warp: the row | entries | hash table
+    int slots;
+};
+__host__ __device__ inline RowLayout row_layout(int cv, int K)
+{
+    RowLayout l;
+    l.ent = (uint32_t)cv * 16u;
+    l.slots = 32;
+    while (l.slots < 2 * K) l.slots *= 2;
+    l.table = l.ent + ((uint32_t)K * kEntryWords + kMaxWarps + 1u) * 4u;
+    l.total = (l.table + 4u * (uint32_t)l.slots + 15u) & ~15u;
+    return l;
+}
+template <int R, bool SHIFT, bool MEAN>
+__global__ void __launch_bounds__(kRowWarps * 32, R <= 4 ? 3 : 2) k_distill_rows(const DistillArgs p, float *loss)
+{
+    pdl_trigger();
+    pdl_wait();
+    extern __shared__ __align__(128) uint8_t smem[];
+    const RowLayout L = row_layout(p.cv, p.K);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint8_t *mine = smem + (size_t)warp * L.total;
+    uint4 *v = (uint4 *)mine;
+    float *at = (float *)(mine + L.ent);
+    const Entries ent = {(int32_t *)at, at + p.K, at + 2 * p.K, at + 3 * p.K, (int32_t *)(at + 4 * p.K), (int32_t *)(at + 5 * p.K)};
+    for (int row = (int)blockIdx.x * kRowWarps + warp; row < p.B; row += (int)gridDim.x * kRowWarps) {
+        const int sh = shift_of<SHIFT>(p, row);
+        const uint16_t *zr = p.z + (size_t)row * p.ldz;
+        ListAhead ahead;
+        ahead.ask(p, row);
+        uint4 x[R];
+#pragma unroll
+        for (int u = 0; u < R; u++) {
+            const int first = (lane + 32 * u) * 8 - sh;
+            if ((!SHIFT || first >= 0) && first + 8 <= p.C) x[u] = __ldcs((const uint4 *)(zr + first));
+            else {
+                uint32_t w[4] = {0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u, 0xFC00FC00u};
+#pragma unroll
+                for (int e = 0; e < 8; e++)
+                    if ((unsigned)(first + e) < (unsigned)p.C)
+                        w[e >> 1] = (e & 1) ? (w[e >> 1] & 0xFFFFu) | ((uint32_t)zr[first + e] << 16) : (w[e >> 1] & 0xFFFF0000u) | zr[first + e];
+                x[u] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        }
+        const bool live = prepare_entries(p, row, 0, sh, ahead, ent, (int *)(mine + L.table), L.slots);
+        __half2 mx = __half2half2(__ushort_as_half((unsigned short)kNegInf16));
+#pragma unroll
+        for (int u = 0; u < R; u++) {
+            if (lane + 32 * u < p.cv) v[lane + 32 * u] = x[u];
+            mx = __hmax2(mx, max8(x[u]));
+        }
+        const float m = fmaxf(__low2float(mx), __high2float(mx));           // NaN is dropped here and comes back in the sum
+        const float b = m == -INFINITY ? 0.0f : -__fmul_rn(m, p.k);
+        float a[4] = {0.0f, 0.0f, 0.0f, 0.0f}, e[R][8];
+#pragma unroll
+        for (int u = 0; u < R; u++) {
+            const uint32_t w[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+            for (int q = 0; q < 4; q++) {
+                const float2 f = __half22float2(*(const __half2 *)&w[q]);
+                e[u][2 * q] = ex2_approx(fmaf(f.x, p.k, b));
+                e[u][2 * q + 1] = ex2_approx(fmaf(f.y, p.k, b));
+                a[q] += e[u][2 * q] + e[u][2 * q + 1];
+            }
+        }
+        const float2 pr = warp_pair(m == -INFINITY ? -INFINITY : -b, (a[0] + a[1]) + (a[2] + a[3]));
+        __syncwarp();
+        keep_targets((const uint16_t *)v, -sh, p.cv * 8, ent, 0);
+        __syncwarp();
+        if (p.dz) {
+            uint16_t *out = p.dz + (size_t)row * p.lddz;
+            const float cs = __fdiv_rn(p.c, pr.y);
+            // this lane's exponentials are relative to 2^-b: a lane of nothing but -inf has zeros (or NaN)
+            const float k = m == -INFINITY ? cs * 0.0f : cs * ex2_approx(-b - pr.x);
+#pragma unroll
+            for (int u = 0; u < R; u++)
+                if (lane + 32 * u < p.cv)
+                    v[lane + 32 * u] = live ? make_uint4(pack_f16x2(e[u][0] * k, e[u][1] * k), pack_f16x2(e[u][2] * k, e[u][3] * k),
+                                                         pack_f16x2(e[u][4] * k, e[u][5] * k), pack_f16x2(e[u][6] * k, e[u][7] * k))
+                                            : make_uint4(0u, 0u, 0u, 0u);
+            __syncwarp();
+            if (live) patch_targets((uint16_t *)v, -sh, p.cv * 8, ent, 0, p.k, pr, cs, p.c);
+            __syncwarp();
+#pragma unroll
+            for (int u = 0; u < R; u++) {
+                const int first = (lane + 32 * u) * 8 - sh;
+                if (lane + 32 * u < p.cv) store8<SHIFT>(out + first, v[lane + 32 * u], first, p.C, p.same);
+            }
+        }
+        write_loss(p, row, ent, live, pr);
+        __syncwarp();                               // the entries are the next row's now
+    }
+    if (MEAN) {
+        __shared__ double red[kRowWarps * 32];
+        cluster_sync_all();                         // every row's loss is there
+        if (blockIdx.x == 0) mean_of_rows(p.row_loss, p.B, loss, red);
+    }
+}
+
 constexpr uint32_t kSmemLimit = 220u * 1024u;
+
+template <int R, bool SHIFT, bool MEAN>
+cudaError_t run_rows(const DistillArgs &p, float *loss, cudaStream_t st)
+{
+    static bool configured[kMaxDevices] = {};
+    const int dev = current_device_slot();
+    if (dev < 0) return cudaErrorInvalidDevice;
+    auto kern = k_distill_rows<R, SHIFT, MEAN>;
+    if (!configured[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit);
+        if (e != cudaSuccess) return e;
+        configured[dev] = true;
+    }
+    const long need = ((long)p.B + kRowWarps - 1) / kRowWarps;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 8;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = MEAN ? 2 : 1;
+    cfg.gridDim = dim3(MEAN ? 8u : (unsigned)(need < 148 * 8 ? need : 148 * 8));
+    cfg.blockDim = dim3(kRowWarps * 32);
+    cfg.dynamicSmemBytes = (size_t)kRowWarps * row_layout(p.cv, p.K).total;
+    cfg.stream = st;
+    return cudaLaunchKernelEx(&cfg, kern, p, loss);
+}
+template <int R, bool SHIFT>
+cudaError_t run_rows_mean(const DistillArgs &p, float *loss, bool mean, cudaStream_t st)
+{
+    return mean ? run_rows<R, SHIFT, true>(p, loss, st) : run_rows<R, SHIFT, false>(p, loss, st);
+}
+template <bool SHIFT>
+cudaError_t launch_rows(const DistillArgs &p, float *loss, bool mean, cudaStream_t st)
+{
+    const int R = (p.cv + 31) / 32;
+    if (R <= 1) return run_rows_mean<1, SHIFT>(p, loss, mean, st);
+    if (R <= 2) return run_rows_mean<2, SHIFT>(p, loss, mean, st);
+    if (R <= 4) return run_rows_mean<4, SHIFT>(p, loss, mean, st);
+    return run_rows_mean<8, SHIFT>(p, loss, mean, st);
+}
 
 typedef void (*DistillKernel)(const DistillArgs);
 
-// id: a number of its own for each kernel (what is known about it is kept per device); extra: warps besides those that
-// hold logits and the teacher's
-cudaError_t run(DistillKernel kern, int id, int extra, const DistillArgs &p, uint32_t smem, cudaStream_t st)
+// id: a number of its own for each kernel (what is known about it is kept per device).
+cudaError_t configure(DistillKernel kern, int id)
 {
-    static bool configured[kMaxDevices][32] = {};
-    static int resident[kMaxDevices][9] = {};       // clusters of a size that the device holds, one CTA per SM; 0 = not asked yet
+    static bool configured[kMaxDevices][16] = {};
     const int dev = current_device_slot();
     if (dev < 0) return cudaErrorInvalidDevice;
-    if (!configured[dev][id]) {
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit);
-        if (e != cudaSuccess) return e;
-        configured[dev][id] = true;
+    if (configured[dev][id]) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemLimit);
+    configured[dev][id] = e == cudaSuccess;
+    return e;
+}
+// Clusters of cl CTAs of the streaming kernel that are resident at once, one CTA on an SM; 0: an error.
+int resident_clusters(DistillKernel kern, int cl)
+{
+    static int resident[kMaxDevices][9] = {};       // 0 = not asked yet
+    const int dev = current_device_slot();
+    if (dev < 0) return 0;
+    if (resident[dev][cl] == 0) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim.x = (unsigned)cl;
+        attr.val.clusterDim.y = 1;
+        attr.val.clusterDim.z = 1;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        cfg.gridDim = dim3((unsigned)(148 / cl * cl));
+        cfg.blockDim = dim3((kMaxWarps + kTeachers) * 32);
+        cfg.dynamicSmemBytes = kSmemLimit;
+        int n = 0;
+        if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) return 0;
+        resident[dev][cl] = n;
     }
+    return resident[dev][cl];
+}
+// Rows are dealt out statically, so a cluster that had to wait for another to end would double the time: no more clusters
+// than are resident at once.  extra: warps besides those that hold logits and the teacher's; most: warps that an SM's registers
+// hold.
+cudaError_t run(DistillKernel kern, int resident, int extra, int most, const DistillArgs &p, uint32_t smem, cudaStream_t st)
+{
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -891,25 +1094,12 @@ cudaError_t run(DistillKernel kern, int id, int extra, const DistillArgs &p, uin
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.stream = st;
     cfg.attrs = attr;
-    // Rows are dealt out statically, so a cluster that had to wait for another to end would double the time: no more
-    // clusters than are resident at once.
-    if (resident[dev][p.cl] == 0) {
-        cfg.gridDim = dim3((unsigned)(148 / p.cl * p.cl));
-        cfg.blockDim = dim3((kMaxWarps + kTeachers + extra) * 32);
-        cfg.dynamicSmemBytes = kSmemLimit;
-        cfg.numAttrs = 1;
-        int n = 0;
-        const cudaError_t e = cudaOccupancyMaxActiveClusters(&n, kern, &cfg);
-        if (e != cudaSuccess) return e;
-        if (n < 1) return cudaErrorLaunchOutOfResources;
-        resident[dev][p.cl] = n;
-    }
     const int threads = (p.nw + kTeachers + extra) * 32;
-    int per_sm = (kMaxWarps + kTeachers + extra) * 32 / threads;          // what the kernel's registers allow
+    int per_sm = most * 32 / threads;
     const int by_smem = (int)((227u * 1024u) / (smem + 1024u));
     if (by_smem < per_sm) per_sm = by_smem;
     if (per_sm < 1) per_sm = 1;
-    int clusters = resident[dev][p.cl] * per_sm;
+    int clusters = resident * per_sm;
     if (clusters > p.B) clusters = p.B;
     cfg.gridDim = dim3((unsigned)(clusters * p.cl));
     cfg.blockDim = dim3((unsigned)threads);
@@ -921,46 +1111,72 @@ cudaError_t run(DistillKernel kern, int id, int extra, const DistillArgs &p, uin
 template <bool SHIFT>
 cudaError_t launch_rounds(int rounds, const DistillArgs &p, uint32_t smem, cudaStream_t st)
 {
-    static const DistillKernel kern[kMaxRounds] = {k_distill<1, SHIFT>, k_distill<2, SHIFT>, k_distill<3, SHIFT>, k_distill<4, SHIFT>,
-                                                   k_distill<5, SHIFT>, k_distill<6, SHIFT>, k_distill<7, SHIFT>, k_distill<8, SHIFT>};
-    return run(kern[rounds - 1], (SHIFT ? kMaxRounds : 0) + rounds - 1, 1, p, smem, st);
+    static const DistillKernel kern[] = {k_distill<4, SHIFT, false>, k_distill<5, SHIFT, false>, k_distill<6, SHIFT, false>,
+                                         k_distill<7, SHIFT, false>, k_distill<8, SHIFT, false>};
+    const bool half = rounds == kMinRounds && p.nw <= kHalfWarps;
+    const DistillKernel k = half ? k_distill<kMinRounds, SHIFT, true> : kern[rounds - kMinRounds];
+    const cudaError_t e = configure(k, (SHIFT ? 8 : 0) + (half ? kMaxRounds - kMinRounds + 1 : rounds - kMinRounds));
+    return e != cudaSuccess ? e : run(k, 148, 1, half ? 2 * (kHalfWarps + kTeachers + 1) : kMaxWarps + kTeachers + 1, p, smem, st);
+}
+// Rows that are read twice: CTAs of a cluster share one.  Rounds of rows times what a row takes, in classes: its share of a CTA
+// and what it costs besides (measured with 131072 classes: 0.138 ns a class and 0.3, 1.0, 1.8 and 2.5 us a row; 512 x 793471
+// takes 434, 366 and 418 us in clusters of 1, 2 and 4, 700 x 131072 takes 90, 102 and 137, 10 x 250000 takes 22, 15 and 12 us
+// in clusters of 2, 4 and 8).
+cudaError_t launch_stream(DistillKernel kern, int id, DistillArgs p, cudaStream_t st)
+{
+    const cudaError_t e = configure(kern, id);
+    if (e != cudaSuccess) return e;
+    constexpr int besides[4] = {2000, 7000, 13000, 18000};
+    double least = 0.0;
+    for (int i = 0; i < 4; i++) {
+        const int n = resident_clusters(kern, 1 << i);
+        if (n == 0) return cudaErrorLaunchOutOfResources;
+        const double cost = (double)((p.B - 1) / n + 1) * ((double)p.C / (1 << i) + besides[i]);
+        if (i == 0 || cost < least) {
+            least = cost;
+            p.cl = 1 << i;
+        }
+    }
+    p.kept = p.cl == 1 && p.dz;
+    p.vp = (p.cv + p.cl - 1) / p.cl;
+    p.wv = (p.vp + kMaxWarps - 1) / kMaxWarps;
+    p.nw = (p.vp + p.wv - 1) / p.wv;
+    p.ns = 3;
+    for (p.per = kChunk; p.per >= 64; p.per -= 64) {      // long teacher lists leave less room
+        const uint32_t smem = layout_of(p.nw, p.ns, p.per, p.cl, p.K, 1 << p.nb_log2).total;
+        if (smem <= kSmemLimit) return run(kern, resident_clusters(kern, p.cl), 0, kMaxWarps + kTeachers, p, smem, st);
+    }
+    return cudaErrorInvalidConfiguration;
 }
 
-cudaError_t launch_distill(DistillArgs p, cudaStream_t st)
+// `loss` receives the mean, too, if the kernel that suits the call takes it (*mean_done).
+cudaError_t launch_distill(DistillArgs p, float *loss, bool *mean_done, cudaStream_t st)
 {
     const bool bulk = (((uintptr_t)p.z | (uintptr_t)p.dz) & 15) == 0 && (p.ldz & 7) == 0 && (!p.dz || (p.lddz & 7) == 0);
     // another pitch or base: the vectors' borders lie elsewhere in every row (all C may be touched by one vector more), and where
     // they lie elsewhere in dz, too, the gradient leaves by elements
     p.same = !p.dz || ((((uintptr_t)p.z ^ (uintptr_t)p.dz) & 15) == 0 && ((p.ldz ^ p.lddz) & 7) == 0);
     const int cv = p.cv = bulk ? (p.C + 7) / 8 : (p.C + 14) / 8;
+    p.cl = p.kept = 1;
+    if (cv <= 256 && p.K <= kRowMaxK) {
+        p.nw = 1;
+        p.vp = p.wv = cv;
+        *mean_done = p.B <= kMeanRows;
+        return bulk ? launch_rows<false>(p, loss, *mean_done, st) : launch_rows<true>(p, loss, *mean_done, st);
+    }
     p.nb_log2 = p.K <= 256 ? 2 : 1;
-    for (p.cl = 1; p.cl <= 8; p.cl *= 2) {
-        p.vp = (cv + p.cl - 1) / p.cl;
-        // few long rows: more SMs per row
-        if (p.cl < 8 && (long)p.B * p.cl * 2 <= 148 && p.vp >= 512) continue;
-        // four vectors a lane where that leaves a row one warp at least, more only where kMaxWarps warps need it
-        int rounds = (p.vp + 32 * kMaxWarps - 1) / (32 * kMaxWarps);
-        if (rounds > kMaxRounds) continue;
-        if (rounds < 4) rounds = p.vp >= 128 ? 4 : (p.vp + 31) / 32;
-        p.wv = p.per = rounds * 32;
-        p.nw = (p.vp + p.wv - 1) / p.wv;
-        for (p.ns = 3; p.ns >= 2; p.ns--) {
-            const uint32_t smem = layout_of(p.nw, p.ns, p.per, p.cl, p.K, 1 << p.nb_log2).total;
-            if (smem <= kSmemLimit) return bulk ? launch_rounds<false>(rounds, p, smem, st) : launch_rounds<true>(rounds, p, smem, st);
-        }
+    // four vectors a lane, more only where kMaxWarps warps need it
+    int rounds = (cv + 32 * kMaxWarps - 1) / (32 * kMaxWarps);
+    if (rounds > kMaxRounds) return bulk ? launch_stream(k_distill_stream<false>, 7, p, st) : launch_stream(k_distill_stream<true>, 15, p, st);
+    if (rounds < kMinRounds) rounds = kMinRounds;
+    p.vp = cv;
+    p.wv = p.per = rounds * 32;
+    p.nw = (cv + p.wv - 1) / p.wv;
+    for (p.ns = 3; p.ns >= 2; p.ns--) {
+        const uint32_t smem = layout_of(p.nw, p.ns, p.per, 1, p.K, 1 << p.nb_log2).total;
+        if (smem <= kSmemLimit) return bulk ? launch_rounds<false>(rounds, p, smem, st) : launch_rounds<true>(rounds, p, smem, st);
     }
-    p.cl = 4;
-    p.vp = (cv + p.cl - 1) / p.cl;
-    p.wv = (p.vp + kMaxWarps - 1) / kMaxWarps;
-    p.nw = (p.vp + p.wv - 1) / p.wv;
-    uint32_t smem = 0;
-    p.ns = 3;
-    for (p.per = kChunk; p.per >= 64; p.per -= 64) {      // long teacher lists leave less room
-        smem = layout_of(p.nw, p.ns, p.per, p.cl, p.K, 1 << p.nb_log2).total;
-        if (smem <= kSmemLimit) break;
-    }
-    if (p.per < 64) return cudaErrorInvalidConfiguration;
-    return bulk ? run(k_distill_stream<false>, 2 * kMaxRounds, 0, p, smem, st) : run(k_distill_stream<true>, 2 * kMaxRounds + 1, 0, p, smem, st);
+    return cudaErrorInvalidConfiguration;
 }
 
 }  // namespace
@@ -980,6 +1196,7 @@ extern "C" int mpt_distill_topk(const uint16_t *z_dev, int ldz, int B, int C, co
     if (ldz < C || (dz_dev && lddz < C) || ldt < K) return MPT_ERR_SHAPE;
     cudaStream_t st = (cudaStream_t)cuda_stream;
     cudaError_t e = cudaSuccess;
+    bool mean_done = false;
     if (B > 0) {
         DistillArgs p = {};
         p.z = z_dev; p.ldz = (size_t)ldz; p.B = B; p.C = C;
@@ -990,8 +1207,8 @@ extern "C" int mpt_distill_topk(const uint16_t *z_dev, int ldz, int B, int C, co
         p.dz = dz_dev; p.lddz = (size_t)lddz;
         p.row_loss = row_loss_dev;
         p.kerr = status_dev;
-        e = launch_distill(p, st);
+        e = launch_distill(p, loss_dev, &mean_done, st);
     }
-    if (e == cudaSuccess) e = launch_loss_mean(row_loss_dev, B, loss_dev, st);
+    if (e == cudaSuccess && !mean_done) e = launch_loss_mean(row_loss_dev, B, loss_dev, st);
     return e == cudaSuccess ? MPT_OK : MPT_ERR_CUDA;
 }

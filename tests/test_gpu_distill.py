@@ -92,7 +92,9 @@ SHAPES = [  # B, C, K, pitch, shift
     (3, 32000, 16, 32000, 0), (80, 36001, 16, 36008, 0), (160, 60000, 16, 60000, 0), (40, 100001, 1000, 100008, 0), (20, 200001, 7, 200008, 0),
     (9, 420000, 12, 420000, 0), (33, 300007, 300, 300008, 0), (20, 1000003, 50, 1000008, 0), (40, 830000, 20, 830000, 0), (40, 500009, 40, 500016, 0), (2, 793471, 128, 793472, 0), (25, 600000, 5, 600000, 1), (30, 700, 1024, 704, 0),
     (6, 400001, 1024, 400008, 0), (70, 262144, 33, 262144, 0), (3, 1, 1, 1, 5), (9, 5, 4, 5, 1), (7, 6, 3, 6, 7), (20, 13, 5, 14, 2), (300, 32001, 64, 32001, 3),
-    (12, 100001, 20, 100001, 6), (5, 793471, 30, 793471, 0), (20, 50257, 9, 50259, 1), (160, 16384, 64, 16384, 0), (1000, 2048, 40, 2048, 0)]
+    (12, 100001, 20, 100001, 6), (5, 793471, 30, 793471, 0), (20, 50257, 9, 50259, 1), (160, 16384, 64, 16384, 0), (1000, 2048, 40, 2048, 0),
+    (150, 40000, 30, 40000, 0), (151, 33001, 1024, 33001, 0), (76, 300001, 20, 300001, 0), (300, 100000, 9, 100000, 0), (3, 2050, 257, 2050, 0), (700, 64, 64, 64, 0),
+    (64, 2048, 256, 2048, 0), (65, 2041, 256, 2041, 2), (40, 2047, 5, 2047, 1), (5, 16385, 300, 16385, 1)]
 
 
 @pytest.mark.parametrize("B,C,K,ld,shift", SHAPES)
