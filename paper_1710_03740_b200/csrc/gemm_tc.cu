@@ -346,6 +346,7 @@ __global__ void __launch_bounds__(256) k_splitk_reduce(const float *__restrict__
         const int row = (int)(i / groups), col = (int)(i % groups) * 8;
         const float *src = partial + (size_t)row * ldp + col;
         float4 a = *(const float4 *)src, b = *(const float4 *)(src + 4);
+#pragma unroll 8                          // loads ahead of the additions, whose order stays
         for (int sp = 1; sp < split_k; sp++) {
             const float *q = src + (size_t)sp * M * ldp;
             const float4 c = *(const float4 *)q, d = *(const float4 *)(q + 4);

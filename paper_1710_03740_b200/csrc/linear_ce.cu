@@ -41,10 +41,12 @@ __device__ __forceinline__ float ex2(float x)
 
 // Row sums from the group sums: sum_g s_g 2^(-b_g) = y 2^x as the pair (x, y), x the largest -b_g, and the row's
 // loss.  The pair stays apart: log2 of large logits' sum as one FP32 number would not resolve p.  Four rows per CTA (a 32-byte
-// sector of `stats` holds one group of four rows), 64 threads a row; fixed order.
+// sector of `stats` holds one group of four rows), THREADS / 4 threads a row (few rows of many groups: 256, else the chain of loads is
+// long: 3 x 136611 10 us); fixed order.
 // xs (null: not wanted) receives x with the rows of ignored labels as zeros: what a padding row holds, NaN
 // perhaps, must not meet its zero gradient in dW's product.
-__global__ void __launch_bounds__(256) k_ce_combine(const float2 *__restrict__ stats, int R, int V, int groups,
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) k_ce_combine(const float2 *__restrict__ stats, int R, int V, int groups,
                                                     const int32_t *__restrict__ labels, const float *__restrict__ zlabel,
                                                     float2 *__restrict__ rowsum, float *__restrict__ row_loss, uint32_t *bad_labels,
                                                     const uint16_t *__restrict__ x, int ldx, int H, uint16_t *__restrict__ xs,
@@ -52,20 +54,21 @@ __global__ void __launch_bounds__(256) k_ce_combine(const float2 *__restrict__ s
 {
     pdl_trigger();
     pdl_wait();
-    __shared__ float2 red[8][4];
+    constexpr int PER_ROW = THREADS / 4;
+    __shared__ float2 red[THREADS / 32][4];
     if (xs) {
-        const int xrow = blockIdx.x * 4 + (threadIdx.x >> 6);
+        const int xrow = blockIdx.x * 4 + threadIdx.x / PER_ROW;
         if (xrow < R) {
             const bool live = (unsigned)labels[xrow] < (unsigned)V;
             const uint4 *src = (const uint4 *)(x + (size_t)xrow * ldx);
             uint4 *dst = (uint4 *)(xs + (size_t)xrow * H);
-            for (int i = threadIdx.x & 63; i < H / 8; i += 64) dst[i] = live ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+            for (int i = threadIdx.x % PER_ROW; i < H / 8; i += PER_ROW) dst[i] = live ? src[i] : make_uint4(0u, 0u, 0u, 0u);
         }
     }
     const int r = threadIdx.x & 3, row = blockIdx.x * 4 + r;
     float m = -INFINITY, s = 0.0f;
     if (row < R) {
-        for (int g = threadIdx.x >> 2; g < groups; g += 64) {
+        for (int g = threadIdx.x >> 2; g < groups; g += PER_ROW) {
             const float2 t = stats[(size_t)g * R + row];
             const float e = -t.y, mn = fmaxf(m, e);         // b is finite, or NaN or -inf where the logits were not
             s = s * ex2(m - mn) + t.x * ex2(e - mn);
@@ -89,7 +92,7 @@ __global__ void __launch_bounds__(256) k_ce_combine(const float2 *__restrict__ s
         m = red[0][r].x;
         s = red[0][r].y;
 #pragma unroll
-        for (int w = 1; w < 8; w++) join(m, s, red[w][r].x, red[w][r].y);
+        for (int w = 1; w < THREADS / 32; w++) join(m, s, red[w][r].x, red[w][r].y);
         const int y = labels[row];
         const bool good = y >= 0 && y < V;
         rowsum[row] = make_float2(m, s);
@@ -107,7 +110,7 @@ __global__ void __launch_bounds__(256) k_ce_combine(const float2 *__restrict__ s
     if (row < R) {
         const float inv = __fdiv_rn(1.0f, s);
         float *f = factor + (size_t)row * groups;
-        for (int g = threadIdx.x >> 2; g < groups; g += 64) f[g] = s == INFINITY ? 0.0f : ex2((-stats[(size_t)g * R + row].y - m) + 14.0f) * inv;
+        for (int g = threadIdx.x >> 2; g < groups; g += PER_ROW) f[g] = s == INFINITY ? 0.0f : ex2((-stats[(size_t)g * R + row].y - m) + 14.0f) * inv;
     }
 }
 
@@ -166,6 +169,131 @@ __global__ void __launch_bounds__(256) k_ce_rescale(uint16_t *__restrict__ e16, 
         }
         *(uint4 *)(er + col) = make_uint4(w[0], w[1], w[2], w[3]);
     }
+}
+
+// dW of few rows, d^T x with a contraction over at most 128 rows: writing dW is what takes time, and the tcgen05 kernels, whose
+// epilogues reach 1.5 to 2.2 TB/s, are bound by that (whole calls of 3 rows, 136611 x 2304: 643 us, with this kernel 390; 64 rows,
+// 50000 x 2048: 229 and 187; 128 rows, 50000 x 1024: 156 and 154).  Here the
+// sums are in registers as they are made (warp-wide mma with FP32 sums: at 16 to 128 terms a sum it costs less than the
+// stores), pass through shared memory and leave in 16-byte stores.  A CTA keeps x for 128 features and goes through the words
+// 128 at a time, the next 128 words' d on the way meanwhile.
+constexpr int kDwRows = 128, kDwTile = 128, kDwPitch = kDwTile + 8;      // pitch: 8 rows of a matrix load lie in different banks
+__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma_16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+constexpr __host__ __device__ int dw_buffers(int steps) { return steps < 8 ? 2 : 1; }      // of d: two CTAs fit on an SM
+constexpr uint32_t dw_smem(int steps) { return (uint32_t)((1 + dw_buffers(steps)) * steps * 16 + 8 * 16) * kDwPitch * 2u; }
+template <int STEPS>
+__global__ void __launch_bounds__(256) k_ce_dw(const uint16_t *__restrict__ d, int ldd, const uint16_t *__restrict__ x, int H, int R, int V,
+                                               float alpha, uint16_t *__restrict__ dW, int lddw, uint32_t *nonfinite_flag, int chunks)
+{
+    extern __shared__ __align__(128) uint8_t smem[];
+    constexpr int K = STEPS * 16, BUFFERS = dw_buffers(STEPS);
+    uint16_t *xt = (uint16_t *)smem, *dt = xt + K * kDwPitch;                   // x | d | a warp's results
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint16_t *out = dt + BUFFERS * K * kDwPitch + warp * 16 * kDwPitch;
+    pdl_trigger();
+    pdl_wait();
+    // rows of a matrix [R, width] from column c0 on, zeros outside
+    auto load = [&](uint16_t *to, const uint16_t *from, int ld, int c0, int width) {
+        for (int i = threadIdx.x; i < K * (kDwTile / 8); i += 256) {
+            const int row = i / (kDwTile / 8), col = i % (kDwTile / 8) * 8;
+            const bool in = row < R && c0 + col < width;
+            const uint32_t dst = (uint32_t)__cvta_generic_to_shared(to + row * kDwPitch + col);
+            const uint16_t *src = in ? from + (size_t)row * ld + c0 + col : from;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    const int h0 = (int)(blockIdx.x % (unsigned)chunks) * kDwTile, tiles = (V + kDwTile - 1) / kDwTile, step = (int)(gridDim.x / (unsigned)chunks);
+    int tile = (int)(blockIdx.x / (unsigned)chunks), at = 0;
+    load(xt, x, H, h0, H);
+    if (tile < tiles) load(dt, d, ldd, tile * kDwTile, ldd);
+    bool bad = false;
+    for (; tile < tiles; tile += step, at ^= BUFFERS - 1) {
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();                         // this tile is there for all, and all are done with the one before
+        if (BUFFERS == 2 && tile + step < tiles) load(dt + (at ^ 1) * K * kDwPitch, d, ldd, (tile + step) * kDwTile, ldd);
+        const uint16_t *dd = dt + at * K * kDwPitch;
+        const int r = lane & 7, m = lane >> 3;
+        float c[kDwTile / 8][4] = {};
+#pragma unroll
+        for (int k = 0; k < STEPS; k++) {
+            uint32_t a[4];
+            ldmatrix_x4_trans(a, (uint32_t)__cvta_generic_to_shared(dd + (k * 16 + (m >> 1) * 8 + r) * kDwPitch + warp * 16 + (m & 1) * 8));
+#pragma unroll
+            for (int n = 0; n < kDwTile / 16; n++) {
+                uint32_t b[4];
+                ldmatrix_x4_trans(b, (uint32_t)__cvta_generic_to_shared(xt + (k * 16 + (m & 1) * 8 + r) * kDwPitch + n * 16 + (m >> 1) * 8));
+                mma_16816(c[2 * n], a, b[0], b[1]);
+                mma_16816(c[2 * n + 1], a, b[2], b[3]);
+            }
+        }
+        if (BUFFERS == 1) {
+            __syncthreads();                     // all have used d
+            if (tile + step < tiles) load(dt, d, ldd, (tile + step) * kDwTile, ldd);
+        }
+        __syncwarp();                            // the last tile's results have left `out`
+#pragma unroll
+        for (int n = 0; n < kDwTile / 8; n++) {
+            const int col = n * 8 + (lane & 3) * 2, row = lane >> 2;
+            *(__half2 *)(out + row * kDwPitch + col) = __floats2half2_rn(c[n][0] * alpha, c[n][1] * alpha);
+            *(__half2 *)(out + (row + 8) * kDwPitch + col) = __floats2half2_rn(c[n][2] * alpha, c[n][3] * alpha);
+        }
+        __syncwarp();
+        const int col = (lane & 15) * 8;
+        if (h0 + col < H) {
+#pragma unroll
+            for (int q = 0; q < 8; q++) {
+                const int row = q * 2 + (lane >> 4), v = tile * kDwTile + warp * 16 + row;
+                const uint4 y = *(const uint4 *)(out + row * kDwPitch + col);
+                if (v < V) {
+                    bad |= half_bits_nonfinite(y.x) || half_bits_nonfinite(y.x >> 16) || half_bits_nonfinite(y.y) || half_bits_nonfinite(y.y >> 16) ||
+                           half_bits_nonfinite(y.z) || half_bits_nonfinite(y.z >> 16) || half_bits_nonfinite(y.w) || half_bits_nonfinite(y.w >> 16);
+                    __stcs((uint4 *)(dW + (size_t)v * lddw + h0 + col), y);
+                }
+            }
+        }
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    if (nonfinite_flag && __any_sync(0xFFFFFFFFu, bad) && lane == 0) atomicOr(nonfinite_flag, 1u);
+}
+template <int STEPS>
+cudaError_t run_dw(int R, int V, int H, const uint16_t *d, int ldd, const uint16_t *x, float alpha, uint16_t *dW, int lddw,
+                   uint32_t *nonfinite_flag, cudaStream_t st)
+{
+    static bool configured[kMaxDevices] = {};
+    const int dev = current_device_slot();
+    if (dev < 0) return cudaErrorInvalidDevice;
+    if (!configured[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(k_ce_dw<STEPS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)dw_smem(STEPS));
+        if (e != cudaSuccess) return e;
+        configured[dev] = true;
+    }
+    const int chunks = (H + kDwTile - 1) / kDwTile, tiles = (V + kDwTile - 1) / kDwTile;
+    // CTAs of neighbouring features work on the same words; about as many CTAs as fit, in whole sets of them, or, where whole
+    // sets leave SMs idle, CTAs of eight tiles each
+    const int fit = 148 * (int)(227u * 1024u / (dw_smem(STEPS) + 1024u));
+    int sets = fit / chunks;
+    if (sets * chunks < fit - fit / 8) sets = (tiles + 7) / 8;
+    if (sets > tiles) sets = tiles;
+    return launch_pdl(k_ce_dw<STEPS>, dim3((unsigned)chunks * (unsigned)sets), dim3(256), dw_smem(STEPS), st, d, ldd, x, H, R, V, alpha, dW, lddw,
+                      nonfinite_flag, chunks);
+}
+cudaError_t launch_dw(int R, int V, int H, const uint16_t *d, int ldd, const uint16_t *x, float alpha, uint16_t *dW, int lddw,
+                      uint32_t *nonfinite_flag, cudaStream_t st)
+{
+    if (R <= 16) return run_dw<1>(R, V, H, d, ldd, x, alpha, dW, lddw, nonfinite_flag, st);
+    if (R <= 32) return run_dw<2>(R, V, H, d, ldd, x, alpha, dW, lddw, nonfinite_flag, st);
+    if (R <= 64) return run_dw<4>(R, V, H, d, ldd, x, alpha, dW, lddw, nonfinite_flag, st);
+    return run_dw<8>(R, V, H, d, ldd, x, alpha, dW, lddw, nonfinite_flag, st);
 }
 
 bool bad_sizes(int N, int V, int H, int row_block)
@@ -259,7 +387,7 @@ Plan make_plan(int N, int V, int H, bool want_dx, bool want_dW, int row_block)
             if (dx_in_launches(rest, H, V) && acc == 0) acc = (size_t)rest * p.ldacc * sizeof(float);
         }
     }
-    if (want_dW && p.blocks == 1) {
+    if (want_dW && p.blocks == 1 && p.R > kDwRows) {
         const size_t s2 = product_scratch(MPT_OP_WGRAD, V, H, p.R);
         sk = s2 > sk ? s2 : sk;
     }
@@ -349,7 +477,8 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
         xl.ce = &ce;
         e = product(MPT_OP_FWD, R, V, H, x, ldx, W_dev, ldw, grads ? e16 : nullptr, p.lde, xl, nullptr, status_dev, nullptr, 0, st);
         if (e != cudaSuccess) break;
-        e = launch_pdl(k_ce_combine, dim3((unsigned)((R + 3) / 4)), dim3(256), 0, st, (const float2 *)stats, R, V, p.groups, labels,
+        const bool wide = p.groups >= 256 && R <= 4 * 148;
+        e = launch_pdl(wide ? k_ce_combine<1024> : k_ce_combine<256>, dim3((unsigned)((R + 3) / 4)), dim3(wide ? 1024 : 256), 0, st, (const float2 *)stats, R, V, p.groups, labels,
                        (const float *)zlabel, rowsum, row_loss_dev + r0, bad_labels_dev, x, ldx, H, xs, factor);
         if (e != cudaSuccess || !grads) continue;
         const bool last = b + 1 == p.blocks;
@@ -386,7 +515,8 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
                 xw.acc_add = b > 0;
                 xw.acc_store = b + 1 < p.blocks;
             }
-            e = product(MPT_OP_WGRAD, V, H, R, e16, p.lde, xs, H, dW_dev, lddw, xw, xw.acc_store ? nullptr : nonfinite_flag_dev,
+            if (p.blocks == 1 && R <= kDwRows) e = launch_dw(R, V, H, e16, p.lde, xs, alpha, dW_dev, lddw, nonfinite_flag_dev, st);
+            else e = product(MPT_OP_WGRAD, V, H, R, e16, p.lde, xs, H, dW_dev, lddw, xw, xw.acc_store ? nullptr : nonfinite_flag_dev,
                         status_dev, ws + p.splitk, p.splitk_bytes, st);
         }
     }

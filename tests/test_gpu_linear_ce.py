@@ -104,7 +104,8 @@ def check(x, W, y, S, got):
 
 SIZES = [(1, 1, 8), (1, 2, 8), (3, 7, 16), (5, 128, 24), (64, 1000, 512), (63, 1001, 520), (128, 129, 64), (129, 257, 72),
          (300, 5003, 256), (700, 20000, 136), (257, 19001, 64), (2, 100003, 64), (130, 40000, 40), (1000, 3001, 1000),
-         (300, 70001, 264), (1024, 200003, 1024), (2048, 70001, 2560), (2050, 33000, 1280)]
+         (300, 70001, 264), (16, 5000, 1000), (17, 129, 136), (32, 20011, 520), (33, 4099, 256), (64, 30003, 128), (65, 6001, 328),
+         (128, 9001, 2048), (7, 131071, 64), (1, 40001, 4096), (1024, 200003, 1024), (2048, 70001, 2560), (2050, 33000, 1280)]
 
 
 @pytest.mark.parametrize("N,V,H", SIZES)
@@ -129,15 +130,16 @@ def test_several_row_blocks(N, V, H, row_block):
 
 
 @pytest.mark.parametrize("grads", ["none", "dx", "dW"])
-@pytest.mark.parametrize("N,V,H", [(100, 513, 64), (400, 15000, 96)])
+@pytest.mark.parametrize("N,V,H", [(100, 513, 64), (400, 15000, 96), (5, 3001, 200)])
 def test_parts_of_the_outputs(N, V, H, grads):
     x, W, y = make(N, V, H, 5)
     got = call(x, W, y, 512.0, grads)
     check(x, W, y, 512.0, got)
 
 
-def test_pitched_rows():
-    x, W, y = make(200, 777, 48, 9)
+@pytest.mark.parametrize("N", [9, 200])
+def test_pitched_rows(N):
+    x, W, y = make(N, 777, 48, 9)
     check(x, W, y, 256.0, call(x, W, y, 256.0, ldx=64, ldw=56))
 
 
