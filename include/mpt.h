@@ -518,10 +518,11 @@ void mpt_lstm_destroy(mpt_lstm_ctx *ctx);
  * workspace: mpt_layernorm_workspace_bytes, 16-byte aligned, owned by the caller and in use until the call's
  * stream work has completed (calls that may overlap need one each).  Results are run-to-run identical.
  * Fastest where all rows and the parameters are 16-byte aligned (base pointers, and pitches that are multiples of 8); rows
- * that are not are shifted on the way (about 1.6 times as long); rows of more than 16384 features forward, 12288 backward, are read more than once (by kernels
- * that keep nothing of a row on chip).  cols from 1 to 2^30, rows from 0 to 2^30 (MPT_ERR_SHAPE otherwise).  Outputs must not overlap inputs (the same pointer is
- * refused).  rows == 0: forward does nothing, backward writes zero dgamma and dbeta.  The stream must belong to
- * the current device (the launch fails otherwise: MPT_ERR_CUDA).  Bytes moved per element: 4 forward, 6 backward. */
+ * that are not are shifted on the way (about 1.6 times as long); rows of more than 16384 features forward, 12288
+ * backward, are read more than once (by kernels that keep nothing of a row on chip).  cols from 1 to 2^30, rows from
+ * 0 to 2^30 (MPT_ERR_SHAPE otherwise).  Outputs must not overlap inputs (the same pointer is refused).  rows == 0:
+ * forward does nothing, backward writes zero dgamma and dbeta.  The stream must belong to the current device (the
+ * launch fails otherwise: MPT_ERR_CUDA).  Bytes moved per element: 4 forward, 6 backward. */
 int mpt_layernorm_forward(int rows, int cols, const uint16_t *x_dev, int ldx, const uint16_t *gamma16_dev,
                           const uint16_t *beta16_dev, float eps, uint16_t *y_dev, int ldy, float *mean_dev, float *rstd_dev,
                           uint32_t *status_dev, void *cuda_stream);
@@ -555,8 +556,8 @@ int mpt_softmax_ce(const uint16_t *z_dev, int ldz, const int32_t *labels_dev, in
  * by some hundreds, however far, has p = 0).
  * x: FP16 [N, H], W: FP16 [V, H], dx like x, dW like W, row-major with pitches in elements; labels: int32 [N]
  * on the device.  A label outside [0, V) contributes neither loss nor gradient, whatever its row of x holds (its
- * row of dx is zero where W is finite; the mean still divides by N).  dx_dev and dW_dev may each be null (not wanted; with both null only the losses are computed
- * and S is ignored).  Gradients are overwritten, not accumulated into.  N == 0: loss 0, dW zero.
+ * row of dx is zero where W is finite; the mean still divides by N).  dx_dev and dW_dev may each be null (not wanted;
+ * with both null only the losses are computed and S is ignored).  Gradients are overwritten, not accumulated into.  N == 0: loss 0, dW zero.
  * bad_labels_dev (may be null): receives the number of labels outside [0, V).  nonfinite_flag_dev (may be null):
  * OR-ed with 1 if any dW is inf or NaN (section 3.2).  status_dev (may be null): one uint32 the caller has zeroed,
  * receives a time-out code if a bounded wait of a product kernel runs out (results are then invalid).

@@ -174,8 +174,8 @@ constexpr int kLnFwdWarps = 24;       // warps of a CTA of the forward kernel
 constexpr __host__ __device__ int ln_bwd_warps(int R) { return R <= 2 ? 16 : 12; }
 // Buffers of a warp: as many as shared memory has room for beside the scale and shift vectors.
 constexpr __host__ __device__ int ln_buffers(int inputs) { return inputs == 1 ? 3 : 4; }
-// Shared memory of a CTA: buffers [warps][ln_buffers][inputs][32 R + 1] of 16 bytes | the scale vector (forward: and the shift vector)
-// [row_warps][32 R] | mbarriers [warps][ln_buffers].
+// Shared memory of a CTA: buffers [warps][ln_buffers][inputs][32 R + 1] of 16 bytes | the scale vector (forward: and the
+// shift vector) [row_warps][32 R] | mbarriers [warps][ln_buffers].
 constexpr __host__ __device__ uint32_t ln_params_at(int warps, int R, int inputs) 
 {
     return (uint32_t)(warps * ln_buffers(inputs) * inputs * (R * 512 + 16));
@@ -202,7 +202,7 @@ struct LnWarp {
     uint32_t *status;
     bool dead = false;
 
-    static constexpr int kPart = R * 32 + 1;        // vectors of an input in a buffer: a part that lies across 16-byte boundaries touches one more
+    static constexpr int kPart = R * 32 + 1;        // vectors of an input in a buffer: a part across 16-byte boundaries touches one more
     static constexpr int kSlot = NIN * kPart;
     static constexpr int kBuffers = ln_buffers(NIN);
 

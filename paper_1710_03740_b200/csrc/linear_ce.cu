@@ -40,9 +40,9 @@ __device__ __forceinline__ float ex2(float x)
 }
 
 // Row sums from the group sums: sum_g s_g 2^(-b_g) = y 2^x as the pair (x, y), x the largest -b_g, and the row's
-// loss.  The pair stays apart: log2 of large logits' sum as one FP32 number would not resolve p.  Four rows per CTA (a 32-byte
-// sector of `stats` holds one group of four rows), THREADS / 4 threads a row (few rows of many groups: 256, else the chain of loads is
-// long: 3 x 136611 10 us); fixed order.
+// loss.  The pair stays apart: log2 of large logits' sum as one FP32 number would not resolve p.  Four rows per CTA (a
+// 32-byte sector of `stats` holds one group of four rows), THREADS / 4 threads a row (few rows of many groups: 256, else
+// the chain of loads is long: 3 x 136611 10 us); fixed order.
 // xs (null: not wanted) receives x with the rows of ignored labels as zeros: what a padding row holds, NaN
 // perhaps, must not meet its zero gradient in dW's product.
 template <int THREADS>
