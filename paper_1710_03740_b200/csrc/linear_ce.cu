@@ -18,7 +18,7 @@
 // 2^-12 of the value whatever S and N: the scale 2^14 leaves 2^-38 of a group's largest term (resp. of 1) above
 // zero, where p * S / N in FP16 would lose p below 2^-24 N / S.  Over several row blocks dW is summed in FP32.
 // Measured: 4096 x 32000 x 12288 7.4-8.5 ms (1.13-1.3 PFLOP/s, under the power cap), 1024 x 793471 x 1024 5.4-6.0 ms,
-// losses alone 2500 x 50001 x 2048 0.41 ms (1.25 PFLOP/s), 64 x 1000 x 512 23 us.
+// losses alone 2500 x 50001 x 2048 0.41 ms (1.25 PFLOP/s), 64 x 1000 x 512 20 us.
 #include <math.h>
 
 #include "mpt_common.cuh"
@@ -37,6 +37,41 @@ __device__ __forceinline__ float ex2(float x)
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// (m, s) pairs, s 2^m each, added; those with m = -inf hold no terms yet.
+__device__ __forceinline__ void join(float &m1, float &s1, float m2, float s2)
+{
+    const float mn = fmaxf(m1, m2);
+    s1 = (m1 == -INFINITY ? 0.0f : s1 * ex2(m1 - mn)) + (m2 == -INFINITY ? 0.0f : s2 * ex2(m2 - mn));
+    m1 = mn;
+}
+// The loss of a row with the sum s 2^m and the label's logit z, in the units of the reference, so that what log2(e) loses as an
+// FP32 number cancels.
+__device__ __forceinline__ float row_loss_of(float m, float s, float z)
+{
+    return (float)(((double)m - (double)z * (double)kLog2e + log2((double)s)) * 0.69314718055994530942);
+}
+// Eight exponentials of a row, the first of class col, to 2^14 (p - [v = y]).
+__device__ __forceinline__ uint4 rescale8(const uint4 v, float f, int y, int col, float z, float2 sum)
+{
+    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+    uint32_t w[4];
+#pragma unroll
+    for (int q = 0; q < 4; q++) {
+        const float2 t = __half22float2(*(const __half2 *)&x[q]);
+        const __half2 h = __floats2half2_rn(t.x * f, t.y * f);
+        w[q] = *(const uint32_t *)&h;
+    }
+    if (y - col >= 0 && y - col < 8) {           // the label's element from its FP32 logit
+        const float p = ex2(fmaf(z, kLog2e, -sum.x)) * __fdiv_rn(1.0f, sum.y);
+        const uint32_t h = (uint32_t)__half_as_ushort(__float2half_rn((p - 1.0f) * 16384.0f));
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            if (((y - col) >> 1) == q) w[q] = ((y - col) & 1) ? ((w[q] & 0x0000FFFFu) | (h << 16)) : ((w[q] & 0xFFFF0000u) | h);
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Row sums from the group sums: sum_g s_g 2^(-b_g) = y 2^x as the pair (x, y), x the largest -b_g, and the row's
@@ -75,12 +110,6 @@ __global__ void __launch_bounds__(THREADS) k_ce_combine(const float2 *__restrict
             m = mn;
         }
     }
-    // (m, s) pairs with m = -inf hold no terms yet
-    auto join = [](float &m1, float &s1, float m2, float s2) {
-        const float mn = fmaxf(m1, m2);
-        s1 = (m1 == -INFINITY ? 0.0f : s1 * ex2(m1 - mn)) + (m2 == -INFINITY ? 0.0f : s2 * ex2(m2 - mn));
-        m1 = mn;
-    };
 #pragma unroll
     for (int o = 4; o < 32; o <<= 1) {
         const float m2 = __shfl_xor_sync(0xFFFFFFFFu, m, o), s2 = __shfl_xor_sync(0xFFFFFFFFu, s, o);
@@ -96,8 +125,7 @@ __global__ void __launch_bounds__(THREADS) k_ce_combine(const float2 *__restrict
         const int y = labels[row];
         const bool good = y >= 0 && y < V;
         rowsum[row] = make_float2(m, s);
-        // the label's logit in the same units as the reference, so that what log2(e) loses as an FP32 number cancels
-        if (good) row_loss[row] = (float)(((double)m - (double)zlabel[row] * (double)kLog2e + log2((double)s)) * 0.69314718055994530942);
+        if (good) row_loss[row] = row_loss_of(m, s, zlabel[row]);
         else row_loss[row] = 0.0f;                      // contributes neither loss nor gradient
         if (!good && bad_labels) atomicAdd(bad_labels, 1u);
         red[0][r] = make_float2(m, good ? s : INFINITY);     // an ignored row's factors are zeros
@@ -148,26 +176,65 @@ __global__ void __launch_bounds__(256) k_ce_rescale(uint16_t *__restrict__ e16, 
     for (int u = 0; u < 8; u++) {
         const int col = col0 + u * 2048;
         if (col >= ld) continue;
-        uint32_t w[4] = {0u, 0u, 0u, 0u};
-        if (good) {
-            const uint32_t x[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+        const bool label = good && y - col >= 0 && y - col < 8;
+        *(uint4 *)(er + col) = good ? rescale8(v[u], f[u], y, col, label ? zlabel[row] : 0.0f, label ? rowsum[row] : make_float2(0.0f, 1.0f))
+                                    : make_uint4(0u, 0u, 0u, 0u);
+    }
+}
+
+// Both passes in one for a few rows of at most 128 groups: a CTA takes a whole row (64 x 1000 x 512: 22.7 us with five launches,
+// 20.1 with four).
+constexpr int kSmallGroups = 128;
+__global__ void __launch_bounds__(256) k_ce_finish(uint16_t *__restrict__ e16, int ld, const float2 *__restrict__ stats, int R, int V, int groups,
+                                                   const int32_t *__restrict__ labels, const float *__restrict__ zlabel,
+                                                   float *__restrict__ row_loss, uint32_t *bad_labels, const uint16_t *__restrict__ x, int ldx,
+                                                   int H, uint16_t *__restrict__ xs)
+{
+    pdl_trigger();
+    pdl_wait();
+    __shared__ float2 red[4];
+    __shared__ float factor[kSmallGroups];
+    const int row = blockIdx.x, t = threadIdx.x, y = labels[row];
+    const bool good = y >= 0 && y < V;
+    uint16_t *er = e16 + (size_t)row * ld;
+    uint4 v[8];
 #pragma unroll
-            for (int q = 0; q < 4; q++) {
-                const float2 t = __half22float2(*(const __half2 *)&x[q]);
-                const __half2 h = __floats2half2_rn(t.x * f[u], t.y * f[u]);
-                w[q] = *(const uint32_t *)&h;
-            }
-            if (y - col >= 0 && y - col < 8) {           // the label's element from its FP32 logit
-                const float2 sum = rowsum[row];
-                const float p = ex2(fmaf(zlabel[row], kLog2e, -sum.x)) * __fdiv_rn(1.0f, sum.y);
-                const uint32_t h = (uint32_t)__half_as_ushort(__float2half_rn((p - 1.0f) * 16384.0f));
+    for (int u = 0; u < 8; u++)
+        if (t * 8 + u * 2048 < ld) v[u] = __ldcs((const uint4 *)(er + t * 8 + u * 2048));
+    const uint4 *src = (const uint4 *)(x + (size_t)row * ldx);
+    uint4 *dst = (uint4 *)(xs + (size_t)row * H);
+    for (int i = t; i < H / 8; i += 256) dst[i] = good ? src[i] : make_uint4(0u, 0u, 0u, 0u);
+    float m = -INFINITY, s = 0.0f, b = 0.0f;
+    if (t < groups) {
+        const float2 st = stats[(size_t)t * R + row];
+        s = st.x;
+        b = st.y;
+        m = -b;
+    }
+    if (t < kSmallGroups) {
 #pragma unroll
-                for (int q = 0; q < 4; q++) {
-                    if (((y - col) >> 1) == q) w[q] = ((y - col) & 1) ? ((w[q] & 0x0000FFFFu) | (h << 16)) : ((w[q] & 0xFFFF0000u) | h);
-                }
-            }
+        for (int o = 1; o < 32; o <<= 1) {
+            const float m2 = __shfl_xor_sync(0xFFFFFFFFu, m, o), s2 = __shfl_xor_sync(0xFFFFFFFFu, s, o);
+            join(m, s, m2, s2);
         }
-        *(uint4 *)(er + col) = make_uint4(w[0], w[1], w[2], w[3]);
+        if ((t & 31) == 0) red[t >> 5] = make_float2(m, s);
+    }
+    __syncthreads();
+    m = red[0].x;
+    s = red[0].y;
+#pragma unroll
+    for (int w = 1; w < kSmallGroups / 32; w++) join(m, s, red[w].x, red[w].y);
+    if (t < groups) factor[t] = ex2((-b - m) + 14.0f) * __fdiv_rn(1.0f, s);
+    if (t == 0) {
+        row_loss[row] = good ? row_loss_of(m, s, zlabel[row]) : 0.0f;
+        if (!good && bad_labels) atomicAdd(bad_labels, 1u);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < 8; u++) {
+        const int col = t * 8 + u * 2048;
+        if (col >= ld) continue;
+        *(uint4 *)(er + col) = good ? rescale8(v[u], factor[col / kGroup], y, col, zlabel[row], make_float2(m, s)) : make_uint4(0u, 0u, 0u, 0u);
     }
 }
 
@@ -192,7 +259,8 @@ constexpr __host__ __device__ int dw_buffers(int steps) { return steps < 8 ? 2 :
 constexpr uint32_t dw_smem(int steps) { return (uint32_t)((1 + dw_buffers(steps)) * steps * 16 + 8 * 16) * kDwPitch * 2u; }
 template <int STEPS>
 __global__ void __launch_bounds__(256) k_ce_dw(const uint16_t *__restrict__ d, int ldd, const uint16_t *__restrict__ x, int H, int R, int V,
-                                               float alpha, uint16_t *__restrict__ dW, int lddw, uint32_t *nonfinite_flag, int chunks)
+                                               float alpha, uint16_t *__restrict__ dW, int lddw, uint32_t *nonfinite_flag, int chunks, int step,
+                                               const float *__restrict__ row_loss, float *__restrict__ loss)
 {
     extern __shared__ __align__(128) uint8_t smem[];
     constexpr int K = STEPS * 16, BUFFERS = dw_buffers(STEPS);
@@ -201,6 +269,10 @@ __global__ void __launch_bounds__(256) k_ce_dw(const uint16_t *__restrict__ d, i
     uint16_t *out = dt + BUFFERS * K * kDwPitch + warp * 16 * kDwPitch;
     pdl_trigger();
     pdl_wait();
+    if (loss && blockIdx.x == gridDim.x - 1) {       // one CTA more than there is work for: the mean loss
+        mean_of_rows(row_loss, R, loss, (double *)smem);
+        return;
+    }
     // rows of a matrix [R, width] from column c0 on, zeros outside
     auto load = [&](uint16_t *to, const uint16_t *from, int ld, int c0, int width) {
         for (int i = threadIdx.x; i < K * (kDwTile / 8); i += 256) {
@@ -212,7 +284,7 @@ __global__ void __launch_bounds__(256) k_ce_dw(const uint16_t *__restrict__ d, i
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    const int h0 = (int)(blockIdx.x % (unsigned)chunks) * kDwTile, tiles = (V + kDwTile - 1) / kDwTile, step = (int)(gridDim.x / (unsigned)chunks);
+    const int h0 = (int)(blockIdx.x % (unsigned)chunks) * kDwTile, tiles = (V + kDwTile - 1) / kDwTile;
     int tile = (int)(blockIdx.x / (unsigned)chunks), at = 0;
     load(xt, x, H, h0, H);
     if (tile < tiles) load(dt, d, ldd, tile * kDwTile, ldd);
@@ -267,7 +339,7 @@ __global__ void __launch_bounds__(256) k_ce_dw(const uint16_t *__restrict__ d, i
 }
 template <int STEPS>
 cudaError_t run_dw(int R, int V, int H, const uint16_t *d, int ldd, const uint16_t *x, float alpha, uint16_t *dW, int lddw,
-                   uint32_t *nonfinite_flag, cudaStream_t st)
+                   uint32_t *nonfinite_flag, const float *row_loss, float *loss, cudaStream_t st)
 {
     static bool configured[kMaxDevices] = {};
     const int dev = current_device_slot();
@@ -284,16 +356,16 @@ cudaError_t run_dw(int R, int V, int H, const uint16_t *d, int ldd, const uint16
     int sets = fit / chunks;
     if (sets * chunks < fit - fit / 8) sets = (tiles + 7) / 8;
     if (sets > tiles) sets = tiles;
-    return launch_pdl(k_ce_dw<STEPS>, dim3((unsigned)chunks * (unsigned)sets), dim3(256), dw_smem(STEPS), st, d, ldd, x, H, R, V, alpha, dW, lddw,
-                      nonfinite_flag, chunks);
+    return launch_pdl(k_ce_dw<STEPS>, dim3((unsigned)chunks * (unsigned)sets + (loss ? 1u : 0u)), dim3(256), dw_smem(STEPS), st, d, ldd, x, H, R,
+                      V, alpha, dW, lddw, nonfinite_flag, chunks, sets, row_loss, loss);
 }
 cudaError_t launch_dw(int R, int V, int H, const uint16_t *d, int ldd, const uint16_t *x, float alpha, uint16_t *dW, int lddw,
-                      uint32_t *nonfinite_flag, cudaStream_t st)
+                      uint32_t *nonfinite_flag, const float *row_loss, float *loss, cudaStream_t st)
 {
-    if (R <= 16) return run_dw<1>(R, V, H, d, ldd, x, alpha, dW, lddw, nonfinite_flag, st);
-    if (R <= 32) return run_dw<2>(R, V, H, d, ldd, x, alpha, dW, lddw, nonfinite_flag, st);
-    if (R <= 64) return run_dw<4>(R, V, H, d, ldd, x, alpha, dW, lddw, nonfinite_flag, st);
-    return run_dw<8>(R, V, H, d, ldd, x, alpha, dW, lddw, nonfinite_flag, st);
+    if (R <= 16) return run_dw<1>(R, V, H, d, ldd, x, alpha, dW, lddw, nonfinite_flag, row_loss, loss, st);
+    if (R <= 32) return run_dw<2>(R, V, H, d, ldd, x, alpha, dW, lddw, nonfinite_flag, row_loss, loss, st);
+    if (R <= 64) return run_dw<4>(R, V, H, d, ldd, x, alpha, dW, lddw, nonfinite_flag, row_loss, loss, st);
+    return run_dw<8>(R, V, H, d, ldd, x, alpha, dW, lddw, nonfinite_flag, row_loss, loss, st);
 }
 
 bool bad_sizes(int N, int V, int H, int row_block)
@@ -477,15 +549,22 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
         xl.ce = &ce;
         e = product(MPT_OP_FWD, R, V, H, x, ldx, W_dev, ldw, grads ? e16 : nullptr, p.lde, xl, nullptr, status_dev, nullptr, 0, st);
         if (e != cudaSuccess) break;
-        const bool wide = p.groups >= 256 && R <= 4 * 148;
-        e = launch_pdl(wide ? k_ce_combine<1024> : k_ce_combine<256>, dim3((unsigned)((R + 3) / 4)), dim3(wide ? 1024 : 256), 0, st, (const float2 *)stats, R, V, p.groups, labels,
-                       (const float *)zlabel, rowsum, row_loss_dev + r0, bad_labels_dev, x, ldx, H, xs, factor);
-        if (e != cudaSuccess || !grads) continue;
-        const bool last = b + 1 == p.blocks;
-        const int chunks = (p.lde + 16383) / 16384;
-        e = launch_pdl(k_ce_rescale, dim3((unsigned)chunks * (unsigned)R + (unsigned)last), dim3(256), 0, st, e16, p.lde,
-                       (const float *)factor, p.groups, V, labels, (const float *)zlabel, (const float2 *)rowsum,
-                       (const float *)row_loss_dev, N, last ? loss_dev : (float *)nullptr, chunks);
+        // the mean loss comes with the rescale pass or, for few rows of few groups, with dW
+        const bool small = dW_dev && p.blocks == 1 && R <= kDwRows && p.groups <= kSmallGroups;
+        if (small) {
+            e = launch_pdl(k_ce_finish, dim3((unsigned)R), dim3(256), 0, st, e16, p.lde, (const float2 *)stats, R, V, p.groups, labels,
+                           (const float *)zlabel, row_loss_dev, bad_labels_dev, x, ldx, H, xs);
+        } else {
+            const bool wide = p.groups >= 256 && R <= 4 * 148;
+            e = launch_pdl(wide ? k_ce_combine<1024> : k_ce_combine<256>, dim3((unsigned)((R + 3) / 4)), dim3(wide ? 1024 : 256), 0, st,
+                           (const float2 *)stats, R, V, p.groups, labels, (const float *)zlabel, rowsum, row_loss_dev + r0, bad_labels_dev, x, ldx, H, xs, factor);
+            if (e != cudaSuccess || !grads) continue;
+            const bool last = b + 1 == p.blocks;
+            const int chunks = (p.lde + 16383) / 16384;
+            e = launch_pdl(k_ce_rescale, dim3((unsigned)chunks * (unsigned)R + (unsigned)last), dim3(256), 0, st, e16, p.lde,
+                           (const float *)factor, p.groups, V, labels, (const float *)zlabel, (const float2 *)rowsum,
+                           (const float *)row_loss_dev, N, last ? loss_dev : (float *)nullptr, chunks);
+        }
         if (e == cudaSuccess && dx_dev) {
             xd.alpha = alpha;
             uint16_t *dx = dx_dev + (size_t)r0 * lddx;
@@ -515,7 +594,8 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
                 xw.acc_add = b > 0;
                 xw.acc_store = b + 1 < p.blocks;
             }
-            if (p.blocks == 1 && R <= kDwRows) e = launch_dw(R, V, H, e16, p.lde, xs, alpha, dW_dev, lddw, nonfinite_flag_dev, st);
+            if (p.blocks == 1 && R <= kDwRows) 
+                e = launch_dw(R, V, H, e16, p.lde, xs, alpha, dW_dev, lddw, nonfinite_flag_dev, row_loss_dev, small ? loss_dev : nullptr, st);
             else e = product(MPT_OP_WGRAD, V, H, R, e16, p.lde, xs, H, dW_dev, lddw, xw, xw.acc_store ? nullptr : nonfinite_flag_dev,
                         status_dev, ws + p.splitk, p.splitk_bytes, st);
         }
