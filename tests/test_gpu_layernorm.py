@@ -112,7 +112,8 @@ SHAPES = [(1, 1, 1, 0), (1, 8, 8, 0), (3, 7, 7, 0), (5, 64, 64, 0), (64, 256, 25
           (150, 1000, 1000, 0), (17, 1024, 1032, 0), (1200, 1024, 1024, 0), (21, 1025, 1032, 0), (40, 2048, 2048, 0),
           (300, 4095, 4096, 0), (31, 6144, 6144, 0), (7, 6145, 6152, 0), (149, 12288, 12288, 0), (5, 12287, 12288, 0),
           (12, 1024, 1024, 3), (6, 5000, 5001, 1), (3, 12296, 12296, 0), (300, 768, 768, 0), (160, 16384, 16384, 0), (33, 15001, 15008, 0), (3, 16392, 16392, 0), (600, 8184, 8192, 0), (5, 8191, 8191, 0), (300, 2047, 2047, 0), (150, 255, 255, 1),
-          (17, 12287, 12287, 5), (4, 1, 1, 3), (6, 9, 9, 1), (5, 5, 6, 7), (600, 1001, 1003, 2), (40, 16383, 16383, 0), (2, 33000, 33000, 0), (5, 40001, 40001, 1)]
+          (17, 12287, 12287, 5), (4, 1, 1, 3), (6, 9, 9, 1), (5, 5, 6, 7), (96, 1024, 1024, 0), (97, 1024, 1024, 0), (8, 12288, 12288, 0), (24, 4096, 4096, 0), (25, 4096, 4096, 0), (3, 9000, 9000, 0),
+          (5, 6000, 6001, 1), (128, 100, 104, 0), (600, 1001, 1003, 2), (40, 16383, 16383, 0), (2, 33000, 33000, 0), (5, 40001, 40001, 1)]
 
 
 @pytest.mark.parametrize("rows,cols", [(1, 3), (7, 30), (310, 1000), (9, 4099), (33, 9001)])
