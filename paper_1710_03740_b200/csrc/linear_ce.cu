@@ -10,9 +10,9 @@
 //   1  the logits product with a softmax epilogue: the accumulators of 128 classes of a row become FP16
 //      exponentials relative to their own maximum (CeEpi), with their FP32 sum, and the label's FP32 logit
 //   2  k_ce_combine: the row's whole sum, and the row's loss (and x without the ignored rows, for step 5)
-//   3  k_ce_rescale: exponentials -> 2^14 (p - [v = y]) in place
+//   3  k_ce_rescale: exponentials -> 2^14 (p - [v = y]) in place (2 and 3 in one, k_ce_finish, for a few short rows)
 //   4  dx = product of those with W, 5 dW = product of their transpose with x, both with the factor S / N * 2^-14
-//      in the epilogue
+//      in the epilogue (up to 128 rows: dW by k_ce_dw)
 // Keeping the exponentials costs 2 bytes a logit of a block and step 3 (4 bytes a logit through HBM: 143/H of the
 // products' time), computing them a second time would cost a fourth product (1/3).  FP16 keeps them, and p, to
 // 2^-12 of the value whatever S and N: the scale 2^14 leaves 2^-38 of a group's largest term (resp. of 1) above
