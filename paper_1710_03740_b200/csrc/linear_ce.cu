@@ -17,7 +17,7 @@
 // products' time), computing them a second time would cost a fourth product (1/3).  FP16 keeps them, and p, to
 // 2^-12 of the value whatever S and N: the scale 2^14 leaves 2^-38 of a group's largest term (resp. of 1) above
 // zero, where p * S / N in FP16 would lose p below 2^-24 N / S.  Over several row blocks dW is summed in FP32.
-// Measured: 4096 x 32000 x 12288 7.4-8.5 ms (1.13-1.3 PFLOP/s, under the power cap), 1024 x 793471 x 1024 5.4-6.0 ms,
+// Measured: 4096 x 32000 x 12288 7.4-8.5 ms (1.13-1.3 PFLOP/s, under the power cap), 1024 x 793471 x 1024 5.4-6.3 ms,
 // losses alone 2500 x 50001 x 2048 0.41 ms (1.25 PFLOP/s), 64 x 1000 x 512 20 us.
 #include <math.h>
 
