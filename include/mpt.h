@@ -551,9 +551,9 @@ int mpt_softmax_ce(const uint16_t *z_dev, int ldz, const int32_t *labels_dev, in
  *   dx[i,:] = rn16(S/N * sum_v d[i,v] * W[v,:])              FP32 sums, S/N applied before the rounding
  *   dW[v,:] = rn16(S/N * sum_i d[i,v] * x[i,:])
  * The two gradients' products take d as FP16 scaled by 2^14 (rounded twice, each time by at most 2^-11 of the
- * value down to d = 2^-28, and kept down to 2^-38), so no d is lost to a small S/N.  Logits may be of any size for the
- * losses, up to 2^27 in magnitude for the gradients (a class whose weights make its logit smaller than the row's largest
- * by some hundreds, however far, has p = 0).
+ * value down to d = 2^-28, and kept down to 2^-38), so no d is lost to a small S/N.  Logits may be of any size (a class whose
+ * weights make its logit smaller than the row's largest by some hundreds, however far, -inf included, has p = 0; where all of a
+ * row's are -inf, or one is +inf, its loss and gradients are NaN).
  * x: FP16 [N, H], W: FP16 [V, H], dx like x, dW like W, row-major with pitches in elements; labels: int32 [N]
  * on the device.  A label outside [0, V) contributes neither loss nor gradient, whatever its row of x holds (its
  * row of dx is zero where W is finite; the mean still divides by N).  dx_dev and dW_dev may each be null (not wanted;

@@ -27,7 +27,7 @@ namespace mpt {
 namespace {
 
 constexpr int kGroup = 128;           // classes of one softmax group (CeEpi)
-constexpr float kLog2e = 1.4426950408889634f;      // as in the softmax epilogue
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kDefaultRows = 4096;    // rows of a block when the caller does not choose
 constexpr int kMaxSize = 1 << 30;     // N and H: what is added to their indexes stays inside 32 bits
 constexpr int kMaxRows = 65536;       // largest block: CTAs of a pass over it stay inside 31 bits
@@ -39,18 +39,17 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-// (m, s) pairs, s 2^m each, added; those with m = -inf hold no terms yet.
+// (m, s) pairs, s e^m each, added.  m = -inf: no terms (s = 0), or only NaN, which stays.
 __device__ __forceinline__ void join(float &m1, float &s1, float m2, float s2)
 {
     const float mn = fmaxf(m1, m2);
-    s1 = (m1 == -INFINITY ? 0.0f : s1 * ex2(m1 - mn)) + (m2 == -INFINITY ? 0.0f : s2 * ex2(m2 - mn));
+    s1 = (m1 == mn ? s1 : s1 * ex2((m1 - mn) * kLog2e)) + (m2 == mn ? s2 : s2 * ex2((m2 - mn) * kLog2e));
     m1 = mn;
 }
-// The loss of a row with the sum s 2^m and the label's logit z, in the units of the reference, so that what log2(e) loses as an
-// FP32 number cancels.
+// The loss of a row with the sum 2^-14 s e^m and the label's logit z: the logits' difference first, whatever their size.
 __device__ __forceinline__ float row_loss_of(float m, float s, float z)
 {
-    return (float)(((double)m - (double)z * (double)kLog2e + log2((double)s)) * 0.69314718055994530942);
+    return (float)((log2((double)s) - 14.0) * 0.69314718055994530942 + ((double)m - (double)z));
 }
 // Eight exponentials of a row, the first of class col, to 2^14 (p - [v = y]).
 __device__ __forceinline__ uint4 rescale8(const uint4 v, float f, int y, int col, float z, float2 sum)
@@ -64,7 +63,7 @@ __device__ __forceinline__ uint4 rescale8(const uint4 v, float f, int y, int col
         w[q] = *(const uint32_t *)&h;
     }
     if (y - col >= 0 && y - col < 8) {           // the label's element from its FP32 logit
-        const float p = ex2(fmaf(z, kLog2e, -sum.x)) * __fdiv_rn(1.0f, sum.y);
+        const float p = ex2(fmaf(z - sum.x, kLog2e, 14.0f)) * __fdiv_rn(1.0f, sum.y);
         const uint32_t h = (uint32_t)__half_as_ushort(__float2half_rn((p - 1.0f) * 16384.0f));
 #pragma unroll
         for (int q = 0; q < 4; q++) {
@@ -74,8 +73,8 @@ __device__ __forceinline__ uint4 rescale8(const uint4 v, float f, int y, int col
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// Row sums from the group sums: sum_g s_g 2^(-b_g) = y 2^x as the pair (x, y), x the largest -b_g, and the row's
-// loss.  The pair stays apart: log2 of large logits' sum as one FP32 number would not resolve p.  Four rows per CTA (a
+// Row sums from the group sums: sum_g s_g e^(m_g) = y e^x as the pair (x, y), x the largest m_g, and the row's
+// loss.  The pair stays apart: the logarithm of large logits' sum as one FP32 number would not resolve p.  Four rows per CTA (a
 // 32-byte sector of `stats` holds one group of four rows), THREADS / 4 threads a row (few rows of many groups: 256, else
 // the chain of loads is long: 3 x 136611 10 us); fixed order.
 // xs (null: not wanted) receives x with the rows of ignored labels as zeros: what a padding row holds, NaN
@@ -105,9 +104,7 @@ __global__ void __launch_bounds__(THREADS) k_ce_combine(const float2 *__restrict
     if (row < R) {
         for (int g = threadIdx.x >> 2; g < groups; g += PER_ROW) {
             const float2 t = stats[(size_t)g * R + row];
-            const float e = -t.y, mn = fmaxf(m, e);         // b is finite, or NaN or -inf where the logits were not
-            s = s * ex2(m - mn) + t.x * ex2(e - mn);
-            m = mn;
+            join(m, s, t.y, t.x);
         }
     }
 #pragma unroll
@@ -138,7 +135,7 @@ __global__ void __launch_bounds__(THREADS) k_ce_combine(const float2 *__restrict
     if (row < R) {
         const float inv = __fdiv_rn(1.0f, s);
         float *f = factor + (size_t)row * groups;
-        for (int g = threadIdx.x >> 2; g < groups; g += PER_ROW) f[g] = s == INFINITY ? 0.0f : ex2((-stats[(size_t)g * R + row].y - m) + 14.0f) * inv;
+        for (int g = threadIdx.x >> 2; g < groups; g += PER_ROW) f[g] = s == INFINITY ? 0.0f : ex2(fmaf(stats[(size_t)g * R + row].y - m, kLog2e, 14.0f)) * inv;
     }
 }
 
@@ -204,13 +201,13 @@ __global__ void __launch_bounds__(256) k_ce_finish(uint16_t *__restrict__ e16, i
     const uint4 *src = (const uint4 *)(x + (size_t)row * ldx);
     uint4 *dst = (uint4 *)(xs + (size_t)row * H);
     for (int i = t; i < H / 8; i += 256) dst[i] = good ? src[i] : make_uint4(0u, 0u, 0u, 0u);
-    float m = -INFINITY, s = 0.0f, b = 0.0f;
+    float m = -INFINITY, s = 0.0f;
     if (t < groups) {
         const float2 st = stats[(size_t)t * R + row];
         s = st.x;
-        b = st.y;
-        m = -b;
+        m = st.y;
     }
+    const float group_m = m;
     if (t < kSmallGroups) {
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -224,7 +221,7 @@ __global__ void __launch_bounds__(256) k_ce_finish(uint16_t *__restrict__ e16, i
     s = red[0].y;
 #pragma unroll
     for (int w = 1; w < kSmallGroups / 32; w++) join(m, s, red[w].x, red[w].y);
-    if (t < groups) factor[t] = ex2((-b - m) + 14.0f) * __fdiv_rn(1.0f, s);
+    if (t < groups) factor[t] = ex2(fmaf(group_m - m, kLog2e, 14.0f)) * __fdiv_rn(1.0f, s);
     if (t == 0) {
         row_loss[row] = good ? row_loss_of(m, s, zlabel[row]) : 0.0f;
         if (!good && bad_labels) atomicAdd(bad_labels, 1u);

@@ -122,13 +122,13 @@ struct LstmEpi {
 };
 
 // Softmax epilogue of a logits product z = x . W^T (linear_ce.cu): the FP32 accumulators of 128 neighbouring
-// classes of a row are turned into exponentials relative to their own maximum, 2^(z*log2e + b) with b = 14 -
-// max*log2e, rounded downwards, so that the largest is 2^14 and FP16 keeps terms down to 2^-38 of it (logits of more than
-// 2^24 in magnitude: 2^(14 - a step of b) and the less).  Their FP32 sum and b go to
-// stats[group][row], the exponentials (rounded to FP16) to the product's output, the label's logit to zlabel[row].
+// classes of a row are turned into exponentials relative to their own maximum, 2^((z - max)*log2e + 14), so that the
+// largest is 2^14 and FP16 keeps terms down to 2^-38 of it.  Their FP32 sum and the maximum (-inf for a group of nothing but
+// -inf, whose sum is 0) go to stats[group][row], the exponentials (rounded to FP16) to the product's output, the label's logit
+// to zlabel[row].
 struct CeEpi {
     const int32_t *labels;    // [M]
-    float2 *stats;            // [ceil(N / 128)][M]: (sum, b)
+    float2 *stats;            // [ceil(N / 128)][M]: (sum, maximum)
     float *zlabel;            // [M]
     int store;                // 0: statistics only, nothing is written to the output
 };

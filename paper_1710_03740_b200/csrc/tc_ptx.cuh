@@ -629,9 +629,9 @@ __device__ __forceinline__ void epilogue_box_store(uint32_t taddr, uint32_t box,
 }
 
 // Softmax epilogue of one thread for one group of 128 classes (see CeEpi): the group's accumulators are read
-// twice from tensor memory (32 at a time), for their maximum and for the exponentials.  Per logit one FMA, one
-// ex2 on the special-function unit, one addition and half a conversion: 16 results per cycle and SM, about 2100
-// cycles for a CTA's 128 x 256 block, under a main loop of 8 k-blocks or more.  BOX: the FP16 exponentials leave
+// twice from tensor memory (32 at a time), for their maximum and for the exponentials.  Per logit a comparison, a
+// subtraction, one FMA, one ex2 on the special-function unit, one addition and half a conversion: the special-function unit's
+// 16 results per cycle and SM are about 2100 cycles for a CTA's 128 x 256 block, under a main loop of 8 k-blocks or more.  BOX: the FP16 exponentials leave
 // through the two shared-memory boxes of the warp and tensor stores (as in epilogue_box_store), otherwise by
 // 16-byte stores of the lane's own row.  V: classes (columns from V on count nothing and are written as zeros up
 // to the next multiple of 8).
@@ -677,9 +677,10 @@ __device__ __forceinline__ void epilogue_ce_group(uint32_t taddr, int col0, int 
             if ((unsigned)at < 32u) e.zlabel[row] = z;
         }
     }
-    // a group of nothing but -inf gets the exponent of a maximum of 0: its terms are zeros, not NaN.  b is rounded
-    // downwards: above 2^24 its steps are more than 1, and an exponential above 2^16 would be infinite in FP16
-    const float b = m == -INFINITY ? 14.0f : __fmaf_rd(-m, LOG2E, 14.0f);
+    // the terms of a group of nothing but -inf are zeros, not NaN (its maximum stays -inf in the statistics).  The maximum is
+    // subtracted before the factor log2(e): as one FP32 exponent it would be known to 2^(e - 24) only, hundreds for the
+    // largest logits
+    const float ref = m == -INFINITY ? 0.0f : m;
     float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 1
     for (int c = 0; c < 4; c++) {
@@ -689,7 +690,7 @@ __device__ __forceinline__ void epilogue_ce_group(uint32_t taddr, int col0, int 
         const int left = V - (col0 + c * 32);
         float x[32];
 #pragma unroll
-        for (int i = 0; i < 32; i++) x[i] = ex2_approx(fmaf(__uint_as_float(r[i]), LOG2E, b));
+        for (int i = 0; i < 32; i++) x[i] = ex2_approx(fmaf(__uint_as_float(r[i]) - ref, LOG2E, 14.0f));
         if (left < 32) {
 #pragma unroll
             for (int i = 0; i < 32; i++)
@@ -730,7 +731,7 @@ __device__ __forceinline__ void epilogue_ce_group(uint32_t taddr, int col0, int 
                     *(uint4 *)(crow + col0 + c * 32 + g8 * 8) = make_uint4(w[4 * g8], w[4 * g8 + 1], w[4 * g8 + 2], w[4 * g8 + 3]);
         }
     }
-    if (row_ok && col0 < V) e.stats[(size_t)(col0 >> 7) * M + row] = make_float2((s4[0] + s4[1]) + (s4[2] + s4[3]), b);
+    if (row_ok && col0 < V) e.stats[(size_t)(col0 >> 7) * M + row] = make_float2((s4[0] + s4[1]) + (s4[2] + s4[3]), m);
 }
 
 // The same load with an L2 eviction-priority hint (policy from l2_policy()).  Operand lines marked
