@@ -267,6 +267,8 @@ struct LnWarp {
                 };
                 if (lo[k] > 0) elements(0);
                 if (hi[k] < touched) elements(touched - 1);
+                // the copy that refills this place some rows later comes after these ordinary stores
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             }
         }
         __syncwarp();
