@@ -522,13 +522,19 @@ struct Cta {
     {
         const int sh = shift(i), g0 = v0 + f;
         uint16_t *h = (uint16_t *)(buf + s * pitch);
-        if (SHIFT && g0 == 0 && lane < sh) h[lane] = (uint16_t)kNegInf16;
-        if ((g0 + n) * 8 - sh > p.C) {               // the last vector, with a shift perhaps one more
+        const bool head = SHIFT && g0 == 0, tail = (g0 + n) * 8 - sh > p.C;
+        if (head && lane < sh) h[lane] = (uint16_t)kNegInf16;
+        if (tail) {                                  // the last vector, with a shift perhaps one more
             for (int g = SHIFT ? max((p.C + sh) / 8, g0) : g0 + n - 1; g < g0 + n; g++)
                 if (lane < 8 && g * 8 - sh + lane >= p.C) h[(g - g0) * 8 + lane] = (uint16_t)kNegInf16;
+        }
+        if (head || tail) {
+            refilled_later();
             __syncwarp();
-        } else if (SHIFT && g0 == 0) __syncwarp();
+        }
     }
+    // After ordinary stores into a buffer, by the lanes that made them: the bulk copy that refills it comes after them.
+    __device__ __forceinline__ static void refilled_later() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
     // Vectors [first, first + n) of row i to dst, which is free; `bar` completes a phase with them.  A vector that is not the
     // row's alone comes with what lies beside the row (mend() replaces that); one that reaches out of the matrix's memory,
     // by elements.
@@ -550,6 +556,7 @@ struct Cta {
         if (a > 0 || b < n) {
             for (int g = 0; g < a; g++) elements(g);
             for (int g = b; g < n; g++) elements(g);
+            refilled_later();
             __syncwarp();                            // the arrival below tells of these, too
         }
         if (lane == 0) {
