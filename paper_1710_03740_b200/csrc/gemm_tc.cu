@@ -64,6 +64,7 @@ struct TcParams {
     float *partial;
     int ldp;
     LstmEpi lstm;   // read only by the LSTM instantiations of the kernel
+    // read only by the instantiations with EXTRA:
     float alpha;    // factor on the FP32 sum before rounding
     float *acc32;   // FP32 sums kept over several launches (ProductExtra), or null
     int ldacc, acc_add, acc_store;
@@ -97,7 +98,9 @@ struct EpiCfg {
     static constexpr int THREADS = 64 + 128 * SETS;
 };
 
-template <bool A_MN, bool B_MN, int BLOCK_N, bool LSTM = false, bool WIDE = false, bool CE = false>
+// EXTRA: factor and FP32 sums over launches (ProductExtra).  An instantiation of its own: as branches in the ordinary products'
+// epilogue they cost small ones 1 to 3 % and the tiny MLP step 6 % (32.8 -> 34.7 us).
+template <bool A_MN, bool B_MN, int BLOCK_N, bool LSTM = false, bool WIDE = false, bool CE = false, bool EXTRA = false>
 __global__ void __launch_bounds__(EpiCfg<LSTM || WIDE>::THREADS, 1)
 k_gemm_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const TcParams p)
 {
@@ -288,15 +291,17 @@ k_gemm_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
                                                      __uint_as_float(r[4 * v + 2]), __uint_as_float(r[4 * v + 3]));
                         }
                     } else if (row_ok && col0 < p.N) {
-                        if (p.acc32) {       // ldacc is a multiple of 32: a started chunk is whole
-                            float *acc = p.acc32 + (size_t)row * p.ldacc + col0;
-                            if (p.acc_add) add_acc32(r, acc);
-                            if (p.acc_store) {
-                                store_acc32(r, acc);
-                                return;
+                        if constexpr (EXTRA) {
+                            if (p.acc32) {       // ldacc is a multiple of 32: a started chunk is whole
+                                float *acc = p.acc32 + (size_t)row * p.ldacc + col0;
+                                if (p.acc_add) add_acc32(r, acc);
+                                if (p.acc_store) {
+                                    store_acc32(r, acc);
+                                    return;
+                                }
                             }
+                            scale32(r, p.alpha);
                         }
-                        scale32(r, p.alpha);
                         epilogue_store32(r, crow, mrow, col0, p.N, p.relu != 0, bad);
                     }
                 };
@@ -430,13 +435,13 @@ bool tc_gemm_supported(int op, int M, int N, int K, const void *A, int lda, cons
     return true;
 }
 
-template <bool A_MN, bool B_MN, int BN, bool LSTM = false, bool WIDE = false, bool CE = false>
+template <bool A_MN, bool B_MN, int BN, bool LSTM = false, bool WIDE = false, bool CE = false, bool EXTRA = false>
 static cudaError_t launch_variant(const CUtensorMap &ta, const CUtensorMap &tb, const TcParams &p, int grid,
                                   cudaStream_t st)
 {
     static bool configured[kMaxDevices] = {};
     constexpr int SMEM_BYTES = TileCfg<BN>::SMEM_BYTES;
-    auto kern = k_gemm_tc<A_MN, B_MN, BN, LSTM, WIDE, CE>;
+    auto kern = k_gemm_tc<A_MN, B_MN, BN, LSTM, WIDE, CE, EXTRA>;
     const int dev = current_device_slot();
     if (dev < 0) return cudaErrorInvalidDevice;
     if (!configured[dev]) {
@@ -474,7 +479,12 @@ static cudaError_t launch_bn(int op, int M, int N, int K, const uint16_t *A, int
     // two epilogue warp sets when a CTA's whole main loop is short (see EpiCfg)
     const long kblocks = ((long)(units + 147) / 148) * ((K + BLOCK_K - 1) / BLOCK_K / p.split_k);
     const bool wide = kblocks <= 160;
-    if (op == MPT_OP_FWD && p.lstm.c_out) e = launch_variant<false, false, BN, true>(ta, tb, p, grid, st);
+    // parts of a split contraction get their factor when they are added
+    const bool extra = p.split_k == 1 && (p.alpha != 1.0f || p.acc32);
+    if (extra && op == MPT_OP_FWD) return cudaErrorInvalidValue;
+    if (extra && op == MPT_OP_DGRAD) e = wide ? launch_variant<false, true, BN, false, true, false, true>(ta, tb, p, grid, st) : launch_variant<false, true, BN, false, false, false, true>(ta, tb, p, grid, st);
+    else if (extra) e = wide ? launch_variant<true, true, BN, false, true, false, true>(ta, tb, p, grid, st) : launch_variant<true, true, BN, false, false, false, true>(ta, tb, p, grid, st);
+    else if (op == MPT_OP_FWD && p.lstm.c_out) e = launch_variant<false, false, BN, true>(ta, tb, p, grid, st);
     else if (op == MPT_OP_FWD) e = wide ? launch_variant<false, false, BN, false, true>(ta, tb, p, grid, st) : launch_variant<false, false, BN>(ta, tb, p, grid, st);
     else if (op == MPT_OP_DGRAD) e = wide ? launch_variant<false, true, BN, false, true>(ta, tb, p, grid, st) : launch_variant<false, true, BN>(ta, tb, p, grid, st);
     else e = wide ? launch_variant<true, true, BN, false, true>(ta, tb, p, grid, st) : launch_variant<true, true, BN>(ta, tb, p, grid, st);

@@ -70,7 +70,8 @@ struct Params {
     // parts in ascending order and applies the epilogue.  split_k == 1: off.
     int split_k;
     // > 0: that many pairs side by side on a tile; all tiles' first parts come first, then their second ones (the tiles of
-    // a part are neighbours and share its operand panels; split_k / split_side parts of a tile follow one another on one pair)
+    // a part are neighbours and share its operand panels; split_k / split_side parts of a tile follow one another on one pair).
+    // Read only by the instantiations with EXTRA
     int split_side;
     float *partial;
     int ldp;
@@ -83,6 +84,7 @@ struct Params {
     int tma_store;                   // output of whole and half tiles through shared memory and tensor stores
     int hint_a, hint_b;              // L2 eviction priority of the operand loads (0 normal, 1 last, 2 first)
     LstmEpi lstm;                    // read only by the LSTM instantiation of the kernel
+    // read only by the instantiations with EXTRA:
     float alpha;                     // factor on the FP32 sum before rounding
     float *acc32;                    // FP32 sums kept over several launches (ProductExtra), or null
     int ldacc, acc_add, acc_store;
@@ -109,6 +111,7 @@ __device__ __forceinline__ void tile_coords(const Params &p, int tile, int &mb, 
     nb = r / gsz;
 }
 
+template <bool EXTRA>
 __device__ __forceinline__ Unit unit_of(const Params &p, int u, int nkb)
 {
     Unit w;
@@ -121,7 +124,7 @@ __device__ __forceinline__ Unit unit_of(const Params &p, int u, int nkb)
     w.tail_slot = -1;
     if (p.split_k > 1) {            // parts of one tile are neighbouring units: they run side by side
         const int tiles = p.tiles_m * p.tiles_n;
-        if (p.split_side > 0) {
+        if (EXTRA && p.split_side > 0) {
             const int q = u / tiles, side = q % p.split_side, seq = q / p.split_side;
             tile = u - q * tiles;
             w.part = side * (p.split_k / p.split_side) + seq;
@@ -165,7 +168,8 @@ struct EpiCfg {
     static constexpr int THREADS = 64 + 128 * SETS;
 };
 
-template <bool A_MN, bool B_MN, bool LSTM = false, bool WIDE = false, bool CE = false>
+// EXTRA: what ProductExtra asks for beside the softmax epilogue, kept out of the ordinary products.
+template <bool A_MN, bool B_MN, bool LSTM = false, bool WIDE = false, bool CE = false, bool EXTRA = false>
 __global__ void __launch_bounds__(EpiCfg<LSTM || WIDE>::THREADS, 1)
 k_gemm_tc2(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
            const __grid_constant__ CUtensorMap tmBh, const __grid_constant__ CUtensorMap tmC, const Params p)
@@ -219,7 +223,7 @@ k_gemm_tc2(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             int tt = 0;
             const uint64_t pol_a = l2_policy(p.hint_a), pol_b = l2_policy(p.hint_b);
             for (int u = pair_id; u < num_units && ok; u += num_pairs, tt++) {
-                const Unit w = unit_of(p, u, nkb);
+                const Unit w = unit_of<EXTRA>(p, u, nkb);
                 // Every other unit of a cluster walks its k-blocks downwards: the operand panels a wave of
                 // tiles has just finished with are the first ones the next wave asks for, while they are
                 // still in L2 (a wave touches about 107 MB of panels, more than L2 keeps).  Measured on
@@ -285,7 +289,7 @@ k_gemm_tc2(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
             unsigned tr_kb = 0;
 #endif
             for (int u = pair_id; u < num_units && ok; u += num_pairs, t++) {
-                const Unit w = unit_of(p, u, nkb);
+                const Unit w = unit_of<EXTRA>(p, u, nkb);
                 const uint32_t idesc = idesc_base | ((uint32_t)(w.width >> 3) << 17);
                 const int buf = t & 1;
                 const uint32_t acc_ph = (t >> 1) & 1u;
@@ -337,7 +341,7 @@ k_gemm_tc2(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
         int t = 0;
         int boxes_sent = 0;          // tensor stores this warp has issued (lane 0 tracks their bulk groups)
         for (int u = pair_id; u < num_units && ok; u += num_pairs, t++) {
-            const Unit w = unit_of(p, u, nkb);
+            const Unit w = unit_of<EXTRA>(p, u, nkb);
             const int buf = t & 1;
             const uint32_t acc_ph = (t >> 1) & 1u;
             const bool got = mbar_wait(accf_bar(buf), acc_ph, abort_flag);
@@ -414,7 +418,7 @@ k_gemm_tc2(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     __syncwarp();
                     const int colb = w.nb * TILE_N + w.n_off + bx * 64;
                     epilogue_box_store(tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * TILE_N + bx * 64), box, &tmC, row0,
-                                       colb, p.M, p.N, p.relu != 0, mrow, row_ok, acc_bits, p.alpha);
+                                       colb, p.M, p.N, p.relu != 0, mrow, row_ok, acc_bits, EXTRA ? p.alpha : 1.0f);
                 }
                 bad |= nonfinite_any(acc_bits);
             } else {
@@ -426,15 +430,17 @@ k_gemm_tc2(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     tc_wait_ld();
                     const int col0 = w.nb * TILE_N + w.n_off + c * 32;
                     if (row_ok && col0 < p.N) {
-                        if (p.acc32) {       // ldacc is a multiple of 32: a started chunk is whole
-                            float *acc = p.acc32 + (size_t)row * p.ldacc + col0;
-                            if (p.acc_add) add_acc32(r, acc);
-                            if (p.acc_store) {
-                                store_acc32(r, acc);
-                                continue;
+                        if constexpr (EXTRA) {
+                            if (p.acc32) {       // ldacc is a multiple of 32: a started chunk is whole
+                                float *acc = p.acc32 + (size_t)row * p.ldacc + col0;
+                                if (p.acc_add) add_acc32(r, acc);
+                                if (p.acc_store) {
+                                    store_acc32(r, acc);
+                                    continue;
+                                }
                             }
+                            scale32(r, p.alpha);
                         }
-                        scale32(r, p.alpha);
                         epilogue_store32(r, crow, mrow, col0, p.N, p.relu != 0, bad);
                     }
                 }
@@ -499,12 +505,12 @@ __global__ void __launch_bounds__(256) k_tail_reduce(const Params p, int first_t
     if (p.nonfinite_flag && __any_sync(0xFFFFFFFFu, bad) && (threadIdx.x & 31) == 0) atomicOr(p.nonfinite_flag, 1u);
 }
 
-template <bool A_MN, bool B_MN, bool LSTM = false, bool WIDE = false, bool CE = false>
+template <bool A_MN, bool B_MN, bool LSTM = false, bool WIDE = false, bool CE = false, bool EXTRA = false>
 static cudaError_t launch_variant(const CUtensorMap &ta, const CUtensorMap &tb, const CUtensorMap &tbh, const CUtensorMap &tc,
                                   Params p, cudaStream_t st)
 {
     static int max_pairs_dev[kMaxDevices] = {};     // 0 = this device not configured yet
-    auto kern = k_gemm_tc2<A_MN, B_MN, LSTM, WIDE, CE>;
+    auto kern = k_gemm_tc2<A_MN, B_MN, LSTM, WIDE, CE, EXTRA>;
     const int dev = current_device_slot();
     if (dev < 0) return cudaErrorInvalidDevice;
     cudaLaunchConfig_t cfg = {};
@@ -736,7 +742,11 @@ cudaError_t launch_gemm_tc2(int op, int M, int N, int K, const uint16_t *A, int 
     const long kblocks = ((units + 73) / 74) * ((K + BLOCK_K - 1) / BLOCK_K / p.split_k);
     const bool wide = kblocks <= 160;
     cudaError_t e;
-    if (op == MPT_OP_FWD) e = wide ? launch_variant<false, false, false, true>(ta, tb, tbh, tcm, p, st) : launch_variant<false, false>(ta, tb, tbh, tcm, p, st);
+    const bool own_sums = x.alpha != 1.0f || x.acc32 || x.split > 0;
+    if (own_sums && op == MPT_OP_FWD) return cudaErrorInvalidValue;
+    if (own_sums && op == MPT_OP_DGRAD) e = wide ? launch_variant<false, true, false, true, false, true>(ta, tb, tbh, tcm, p, st) : launch_variant<false, true, false, false, false, true>(ta, tb, tbh, tcm, p, st);
+    else if (own_sums) e = wide ? launch_variant<true, true, false, true, false, true>(ta, tb, tbh, tcm, p, st) : launch_variant<true, true, false, false, false, true>(ta, tb, tbh, tcm, p, st);
+    else if (op == MPT_OP_FWD) e = wide ? launch_variant<false, false, false, true>(ta, tb, tbh, tcm, p, st) : launch_variant<false, false>(ta, tb, tbh, tcm, p, st);
     else if (op == MPT_OP_DGRAD) e = wide ? launch_variant<false, true, false, true>(ta, tb, tbh, tcm, p, st) : launch_variant<false, true>(ta, tb, tbh, tcm, p, st);
     else e = wide ? launch_variant<true, true, false, true>(ta, tb, tbh, tcm, p, st) : launch_variant<true, true>(ta, tb, tbh, tcm, p, st);
     if (e != cudaSuccess || p.split_k == 1) return e;

@@ -69,7 +69,7 @@ struct Params {
     uint32_t *nonfinite_flag;
     uint32_t *status;
     int tiles_m, tiles_n;
-    float alpha;                    // factor on the FP32 sum before rounding
+    float alpha;                    // factor on the FP32 sum before rounding (read only by the instantiations with EXTRA)
 };
 
 __device__ __forceinline__ void report(const Params &p, volatile uint32_t *abort_flag, uint32_t code)
@@ -97,7 +97,7 @@ __device__ __forceinline__ void report(const Params &p, volatile uint32_t *abort
 #endif
 
 // S: CTA pairs per cluster = parts of the contraction.  W = 256 / S columns per pair, W / 2 per warp.
-template <bool A_MN, bool B_MN, int S>
+template <bool A_MN, bool B_MN, int S, bool EXTRA = false>
 __global__ void __launch_bounds__(THREADS, 1)
 k_gemm_tc4(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Params p)
 {
@@ -336,7 +336,7 @@ k_gemm_tc4(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
                     }
 #pragma unroll
                     for (int e = 0; e < 32; e++) r[e] = __float_as_uint(sum[e]);
-                    scale32(r, p.alpha);
+                    if constexpr (EXTRA) scale32(r, p.alpha);
                     const int col0 = nb * TILE_N + g * W + set * WCOLS + c * 32;
                     epilogue_store32_coalesced(r, base_ptr + RECV_BYTES + SEND_BYTES + w * EPI_STAGE_BYTES, p.C, p.ldc, p.mask, p.ldmask,
                                                mb * (2 * CTA_M) + (int)half * CTA_M + q * 32, col0, p.M, p.N, p.relu != 0, bad);
@@ -359,11 +359,11 @@ k_gemm_tc4(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUte
     }
 }
 
-template <bool A_MN, bool B_MN, int S>
+template <bool A_MN, bool B_MN, int S, bool EXTRA = false>
 static cudaError_t launch_variant(const CUtensorMap &ta, const CUtensorMap &tb, const Params &p, cudaStream_t st)
 {
     static int max_clusters_dev[kMaxDevices] = {};     // 0 = this device not configured yet, < 0 = cannot run here
-    auto kern = k_gemm_tc4<A_MN, B_MN, S>;
+    auto kern = k_gemm_tc4<A_MN, B_MN, S, EXTRA>;
     const int dev = current_device_slot();
     if (dev < 0) return cudaErrorInvalidDevice;
     cudaLaunchConfig_t cfg = {};
@@ -477,6 +477,11 @@ cudaError_t launch_gemm_tc4(int op, int M, int N, int K, const uint16_t *A, int 
     p.tiles_m = (M + 2 * CTA_M - 1) / (2 * CTA_M);
     p.tiles_n = (N + TILE_N - 1) / TILE_N;
     p.alpha = alpha;
+    if (alpha != 1.0f) {
+        if (op == MPT_OP_FWD) return cudaErrorInvalidValue;
+        if (split == 2) return op == MPT_OP_DGRAD ? launch_variant<false, true, 2, true>(ta, tb, p, st) : launch_variant<true, true, 2, true>(ta, tb, p, st);
+        return op == MPT_OP_DGRAD ? launch_variant<false, true, 4, true>(ta, tb, p, st) : launch_variant<true, true, 4, true>(ta, tb, p, st);
+    }
     if (split == 2) {
         if (op == MPT_OP_FWD) return launch_variant<false, false, 2>(ta, tb, p, st);
         if (op == MPT_OP_DGRAD) return launch_variant<false, true, 2>(ta, tb, p, st);

@@ -184,7 +184,7 @@ __device__ __forceinline__ uint32_t mask_pair(uint32_t w, uint32_t mw)
 __device__ __forceinline__ void nonfinite_acc(uint32_t w, uint32_t &acc) { acc |= (w & 0x7C007C00u) + 0x04000400u; }
 __device__ __forceinline__ bool nonfinite_any(uint32_t acc) { return (acc & 0x80008000u) != 0; }
 
-// Factor on 32 FP32 sums before rounding; 1 (every ordinary product) costs one uniform branch.
+// Factor on 32 FP32 sums before rounding.
 __device__ __forceinline__ void scale32(uint32_t (&r)[32], float alpha)
 {
     if (alpha != 1.0f) {
