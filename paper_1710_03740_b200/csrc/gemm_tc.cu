@@ -337,6 +337,8 @@ k_gemm_tc(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUten
 
 // Second step of a split-K product: C = epilogue(partial[0] + partial[1] + ... ) with the parts
 // added in ascending order (FP32, one rounding per add), eight columns per thread.
+// MANY: more parts than an ordinary product is cut into; eight parts' loads ahead of their additions, whose order stays.
+template <bool MANY>
 __global__ void __launch_bounds__(256) k_splitk_reduce(const float *__restrict__ partial, int split_k, int M, int N,
                                                        int ldp, uint16_t *__restrict__ C, int ldc, int relu,
                                                        const uint16_t *__restrict__ mask, int ldmask,
@@ -351,7 +353,7 @@ __global__ void __launch_bounds__(256) k_splitk_reduce(const float *__restrict__
         const int row = (int)(i / groups), col = (int)(i % groups) * 8;
         const float *src = partial + (size_t)row * ldp + col;
         float4 a = *(const float4 *)src, b = *(const float4 *)(src + 4);
-#pragma unroll 8                          // loads ahead of the additions, whose order stays
+#pragma unroll (MANY ? 8 : 4)
         for (int sp = 1; sp < split_k; sp++) {
             const float *q = src + (size_t)sp * M * ldp;
             const float4 c = *(const float4 *)q, d = *(const float4 *)(q + 4);
@@ -382,7 +384,8 @@ cudaError_t launch_splitk_reduce(const float *partial, int split_k, int M, int N
     const size_t work = (size_t)M * ((N + 7) / 8);
     size_t blocks = (work + 255) / 256;
     if (blocks > 148 * 16) blocks = 148 * 16;
-    MPT_LAUNCH(k_splitk_reduce, dim3((unsigned)blocks), dim3(256), 0, st, partial, split_k, M, N, ldp, C, ldc, relu ? 1 : 0, mask, ldmask,
+    auto kern = split_k > 8 ? k_splitk_reduce<true> : k_splitk_reduce<false>;
+    MPT_LAUNCH(kern, dim3((unsigned)blocks), dim3(256), 0, st, partial, split_k, M, N, ldp, C, ldc, relu ? 1 : 0, mask, ldmask,
                nonfinite_flag, alpha);
     g_last_gemm_launches = 2;
     return cudaGetLastError();

@@ -88,7 +88,6 @@ inline cudaError_t launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, siz
 __device__ __forceinline__ void mean_of_rows(const float *row_loss, int B, float *loss, double *red)
 {
     double acc = 0.0;
-#pragma unroll 8                              // loads ahead of the additions, whose order stays
     for (unsigned i = threadIdx.x; i < (unsigned)B; i += 256) acc += (double)row_loss[i];
     red[threadIdx.x] = acc;
     __syncthreads();
