@@ -18,6 +18,7 @@
 // distributed shared memory.
 #include <math.h>
 
+#include "distill_plan.h"
 #include "mpt_common.cuh"
 #include "tc_ptx.cuh"
 
@@ -1062,29 +1063,26 @@ cudaError_t configure(DistillKernel kern, int id)
     configured[dev][id] = e == cudaSuccess;
     return e;
 }
-// Clusters of cl CTAs of the streaming kernel that are resident at once, one CTA on an SM; 0: an error.
+// Clusters of cl CTAs of the streaming kernel that are resident at once, one CTA on an SM; -1: an error.
 int resident_clusters(DistillKernel kern, int cl)
 {
-    static int resident[kMaxDevices][9] = {};       // 0 = not asked yet
-    const int dev = current_device_slot();
-    if (dev < 0) return 0;
-    if (resident[dev][cl] == 0) {
-        cudaLaunchConfig_t cfg = {};
-        cudaLaunchAttribute attr;
-        attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim.x = (unsigned)cl;
-        attr.val.clusterDim.y = 1;
-        attr.val.clusterDim.z = 1;
-        cfg.attrs = &attr;
-        cfg.numAttrs = 1;
-        cfg.gridDim = dim3((unsigned)(148 / cl * cl));
-        cfg.blockDim = dim3((kMaxWarps + kTeachers) * 32);
-        cfg.dynamicSmemBytes = kSmemLimit;
-        int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess || n < 1) return 0;
-        resident[dev][cl] = n;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)cl;
+    attr.val.clusterDim.y = 1;
+    attr.val.clusterDim.z = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    cfg.gridDim = dim3((unsigned)(148 / cl * cl));
+    cfg.blockDim = dim3((kMaxWarps + kTeachers) * 32);
+    cfg.dynamicSmemBytes = kSmemLimit;
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kern, &cfg) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return -1;
     }
-    return resident[dev][cl];
+    return n;
 }
 // Rows are dealt out statically, so a cluster that had to wait for another to end would double the time: no more clusters
 // than are resident at once.  extra: warps besides those that hold logits and the teacher's; most: warps that an SM's registers
@@ -1125,25 +1123,19 @@ cudaError_t launch_rounds(int rounds, const DistillArgs &p, uint32_t smem, cudaS
     const cudaError_t e = configure(k, (SHIFT ? 8 : 0) + (half ? kMaxRounds - kMinRounds + 1 : rounds - kMinRounds));
     return e != cudaSuccess ? e : run(k, 148, 1, half ? 2 * (kHalfWarps + kTeachers + 1) : kMaxWarps + kTeachers + 1, p, smem, st);
 }
-// Rows that are read twice: CTAs of a cluster share one.  Rounds of rows times what a row takes, in classes: its share of a CTA
-// and what it costs besides (measured with 131072 classes: 0.138 ns a class and 0.3, 1.0, 1.8 and 2.5 us a row; 512 x 793471
-// takes 434, 366 and 418 us in clusters of 1, 2 and 4, 700 x 131072 takes 90, 102 and 137, 10 x 250000 takes 22, 15 and 12 us
-// in clusters of 2, 4 and 8).
-cudaError_t launch_stream(DistillKernel kern, int id, DistillArgs p, cudaStream_t st)
+// Rows that are read twice: CTAs of a cluster share one (distill_cluster_log2).
+template <bool SHIFT>
+cudaError_t launch_stream(DistillArgs p, cudaStream_t st)
 {
-    const cudaError_t e = configure(kern, id);
+    const DistillKernel kern = k_distill_stream<SHIFT>;
+    static int known[kMaxDevices][kDistillClusters] = {};      // of this kernel
+    const int dev = current_device_slot();
+    if (dev < 0) return cudaErrorInvalidDevice;
+    const cudaError_t e = configure(kern, SHIFT ? 15 : 7);
     if (e != cudaSuccess) return e;
-    constexpr int besides[4] = {2000, 7000, 13000, 18000};
-    double least = 0.0;
-    for (int i = 0; i < 4; i++) {
-        const int n = resident_clusters(kern, 1 << i);
-        if (n == 0) return cudaErrorLaunchOutOfResources;
-        const double cost = (double)((p.B - 1) / n + 1) * ((double)p.C / (1 << i) + besides[i]);
-        if (i == 0 || cost < least) {
-            least = cost;
-            p.cl = 1 << i;
-        }
-    }
+    const int size = distill_cluster_log2(known[dev], p.B, p.C, [&](int cl) { return resident_clusters(kern, cl); });
+    if (size < 0) return cudaErrorLaunchOutOfResources;
+    p.cl = 1 << size;
     p.kept = p.cl == 1 && p.dz;
     p.vp = (p.cv + p.cl - 1) / p.cl;
     p.wv = (p.vp + kMaxWarps - 1) / kMaxWarps;
@@ -1151,7 +1143,7 @@ cudaError_t launch_stream(DistillKernel kern, int id, DistillArgs p, cudaStream_
     p.ns = 3;
     for (p.per = kChunk; p.per >= 64; p.per -= 64) {      // long teacher lists leave less room
         const uint32_t smem = layout_of(p.nw, p.ns, p.per, p.cl, p.K, 1 << p.nb_log2).total;
-        if (smem <= kSmemLimit) return run(kern, resident_clusters(kern, p.cl), 0, kMaxWarps + kTeachers, p, smem, st);
+        if (smem <= kSmemLimit) return run(kern, known[dev][size], 0, kMaxWarps + kTeachers, p, smem, st);
     }
     return cudaErrorInvalidConfiguration;
 }
@@ -1174,7 +1166,7 @@ cudaError_t launch_distill(DistillArgs p, float *loss, bool *mean_done, cudaStre
     p.nb_log2 = p.K <= 256 ? 2 : 1;
     // four vectors a lane, more only where kMaxWarps warps need it
     int rounds = (cv + 32 * kMaxWarps - 1) / (32 * kMaxWarps);
-    if (rounds > kMaxRounds) return bulk ? launch_stream(k_distill_stream<false>, 7, p, st) : launch_stream(k_distill_stream<true>, 15, p, st);
+    if (rounds > kMaxRounds) return bulk ? launch_stream<false>(p, st) : launch_stream<true>(p, st);
     if (rounds < kMinRounds) rounds = kMinRounds;
     p.vp = cv;
     p.wv = p.per = rounds * 32;
