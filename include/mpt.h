@@ -521,7 +521,7 @@ void mpt_lstm_destroy(mpt_lstm_ctx *ctx);
  * that are not are shifted on the way (about 1.6 times as long); rows of more than 16384 features forward, 12288
  * backward, are read more than once (by kernels that keep nothing of a row on chip).  cols from 1 to 2^30, rows from
  * 0 to 2^30 (MPT_ERR_SHAPE otherwise).  Outputs must not overlap inputs (the same pointer is refused).  rows == 0:
- * forward does nothing, backward writes zero dgamma and dbeta.  The stream must belong to the current device (the
+ * forward does nothing, backward writes zero dgamma and dbeta, and what holds rows may be null.  The stream must belong to the current device (the
  * launch fails otherwise: MPT_ERR_CUDA).  Bytes moved per element: 4 forward, 6 backward. */
 int mpt_layernorm_forward(int rows, int cols, const uint16_t *x_dev, int ldx, const uint16_t *gamma16_dev,
                           const uint16_t *beta16_dev, float eps, uint16_t *y_dev, int ldy, float *mean_dev, float *rstd_dev,
@@ -557,7 +557,8 @@ int mpt_softmax_ce(const uint16_t *z_dev, int ldz, const int32_t *labels_dev, in
  * x: FP16 [N, H], W: FP16 [V, H], dx like x, dW like W, row-major with pitches in elements; labels: int32 [N]
  * on the device.  A label outside [0, V) contributes neither loss nor gradient, whatever its row of x holds (its
  * row of dx is zero where W is finite; the mean still divides by N).  dx_dev and dW_dev may each be null (not wanted;
- * with both null only the losses are computed and S is ignored).  Gradients are overwritten, not accumulated into.  N == 0: loss 0, dW zero.
+ * with both null only the losses are computed and S is ignored).  Gradients are overwritten, not accumulated into.  N == 0: loss 0, dW
+ * zero, and what holds rows may be null.
  * bad_labels_dev (may be null): receives the number of labels outside [0, V).  nonfinite_flag_dev (may be null):
  * OR-ed with 1 if any dW is inf or NaN (section 3.2).  status_dev (may be null): one uint32 the caller has zeroed,
  * receives a time-out code if a bounded wait of a product kernel runs out (results are then invalid).
@@ -590,7 +591,8 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
  * null (losses only; lddz is then ignored).  To mix with a hard label, call mpt_softmax_ce with the other share of S
  * and add the two gradients (mpt_add_f16).
  * status_dev (may be null): one uint32 the caller has zeroed, receives a time-out code if a bounded wait runs out
- * (results are then invalid).  z and dz must not overlap.  0 <= B <= 2^30, 1 <= C <= MPT_DISTILL_MAX_C, 1 <= K <=
+ * (results are then invalid).  z and dz must not overlap.  0 <= B <= 2^30 (0: loss 0, and what holds
+ * rows may be null), 1 <= C <= MPT_DISTILL_MAX_C, 1 <= K <=
  * MPT_DISTILL_MAX_K; tau from 2^-14 to 2^14 (beyond, exponents of the largest FP16 logits, or tau^2 times a rounding, are not
  * resolved in FP32: MPT_ERR_INVALID_ARG); rows may lie to 16-byte boundaries as they like, if those of
  * dz lie as those of z do (otherwise the gradient leaves element by element).

@@ -1187,7 +1187,8 @@ extern "C" int mpt_distill_topk(const uint16_t *z_dev, int ldz, int B, int C, co
                                 int ldt, int K, float tau, float S, uint16_t *dz_dev, int lddz, float *row_loss_dev,
                                 float *loss_dev, uint32_t *status_dev, void *cuda_stream)
 {
-    if (!z_dev || !t16_dev || !idx_dev || !row_loss_dev || !loss_dev || z_dev == dz_dev) return MPT_ERR_INVALID_ARG;
+    // an empty batch has no addresses: what holds rows may be null then
+    if (!loss_dev || (B != 0 && (!z_dev || !t16_dev || !idx_dev || !row_loss_dev || z_dev == dz_dev))) return MPT_ERR_INVALID_ARG;
     // 65504 log2(e) / tau stays below 2^31, where rounding an exponent's reference is off by 64: sums relative to it cannot
     // overflow
     if (!(tau >= 0x1p-14f && tau <= 0x1p14f) || !isfinite(S)) return MPT_ERR_INVALID_ARG;

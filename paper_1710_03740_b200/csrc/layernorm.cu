@@ -920,7 +920,8 @@ int mpt_layernorm_forward(int rows, int cols, const uint16_t *x_dev, int ldx, co
                           const uint16_t *beta16_dev, float eps, uint16_t *y_dev, int ldy, float *mean_dev, float *rstd_dev,
                           uint32_t *status_dev, void *cuda_stream)
 {
-    if (!x_dev || !gamma16_dev || !y_dev || x_dev == y_dev) return MPT_ERR_INVALID_ARG;
+    // an empty batch has no addresses: what holds rows may be null then, here and in the backward pass
+    if (!gamma16_dev || (rows != 0 && (!x_dev || !y_dev || x_dev == y_dev))) return MPT_ERR_INVALID_ARG;
     if (!(eps >= 0.0f) || !isfinite(eps)) return MPT_ERR_INVALID_ARG;
     if (rows < 0 || rows > kLnMaxSize || cols < 1 || cols > kLnMaxSize || ldx < cols || ldy < cols) return MPT_ERR_SHAPE;
     cudaStream_t st = (cudaStream_t)cuda_stream;
@@ -942,9 +943,8 @@ int mpt_layernorm_backward(int rows, int cols, const uint16_t *dy_dev, int lddy,
                            uint16_t *dgamma16_dev, uint16_t *dbeta16_dev, uint32_t *nonfinite_flag_dev, uint32_t *status_dev,
                            void *workspace_dev, size_t workspace_bytes, void *cuda_stream)
 {
-    if (!dy_dev || !x_dev || !gamma16_dev || !mean_dev || !rstd_dev || !dx_dev || !dgamma16_dev || !workspace_dev)
-        return MPT_ERR_INVALID_ARG;
-    if (dx_dev == dy_dev || dx_dev == x_dev) return MPT_ERR_INVALID_ARG;
+    if (!gamma16_dev || !dgamma16_dev || !workspace_dev) return MPT_ERR_INVALID_ARG;
+    if (rows != 0 && (!dy_dev || !x_dev || !mean_dev || !rstd_dev || !dx_dev || dx_dev == dy_dev || dx_dev == x_dev)) return MPT_ERR_INVALID_ARG;
     if (rows < 0 || rows > kLnMaxSize || cols < 1 || cols > kLnMaxSize || lddy < cols || ldx < cols || lddx < cols) return MPT_ERR_SHAPE;
     size_t need = 0;
     mpt_layernorm_workspace_bytes(rows, cols, &need);

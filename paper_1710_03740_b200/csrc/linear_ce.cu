@@ -516,8 +516,9 @@ int mpt_linear_ce(int N, int V, int H, const uint16_t *x_dev, int ldx, const uin
                   float *loss_dev, uint32_t *bad_labels_dev, uint32_t *nonfinite_flag_dev, uint32_t *status_dev,
                   void *workspace_dev, size_t workspace_bytes, void *cuda_stream)
 {
-    if (!x_dev || !W_dev || !labels_dev || !row_loss_dev || !loss_dev || !workspace_dev) return MPT_ERR_INVALID_ARG;
-    if (((dx_dev || dW_dev) && !isfinite(S)) || dx_dev == x_dev || dW_dev == W_dev) return MPT_ERR_INVALID_ARG;
+    // an empty batch has no addresses: what holds rows may be null then
+    if (!W_dev || !loss_dev || !workspace_dev || (N != 0 && (!x_dev || !labels_dev || !row_loss_dev || dx_dev == x_dev))) return MPT_ERR_INVALID_ARG;
+    if (((dx_dev || dW_dev) && !isfinite(S)) || dW_dev == W_dev) return MPT_ERR_INVALID_ARG;
     if (bad_sizes(N, V, H, row_block)) return MPT_ERR_SHAPE;
     if (ldx < H || ldw < H || (dx_dev && lddx < H) || (dW_dev && lddw < H)) return MPT_ERR_SHAPE;
     const uintptr_t bits = (uintptr_t)x_dev | (uintptr_t)W_dev | (uintptr_t)dx_dev | (uintptr_t)dW_dev;

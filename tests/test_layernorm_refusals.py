@@ -68,3 +68,11 @@ def test_binding_refuses_host_tensors(lib):
 
     with pytest.raises(ValueError):
         binding.mpt_layernorm_forward(1, 64, t, 64, t, None, 1e-5, t, 64, stream=FakeStream())
+
+
+def test_an_empty_batch_may_come_without_addresses(lib):
+    assert fwd(lib, rows=0, x=None, y=None) == 0          # nothing is launched
+    assert fwd(lib, rows=0, x=None, y=None, gamma=None) == INVALID
+    assert bwd(lib, rows=0, dy=None, x=None, mean=None, rstd=None, dx=None, dgamma=None) == INVALID
+    assert bwd(lib, rows=0, dy=None, x=None, mean=None, rstd=None, dx=None, ws=None) == INVALID
+    assert bwd(lib, rows=-1, dy=None) == INVALID and fwd(lib, rows=-1) == SHAPE
