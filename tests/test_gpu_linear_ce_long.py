@@ -52,3 +52,19 @@ def test_row_blocks_with_long_contractions(N, V, H, row_block):
     y[::9] = -1
     S = 2.0 ** (2 + N.bit_length())
     check(x, W, y, S, call(x, W, y, S, row_block=row_block))
+
+
+@pytest.mark.parametrize("N,V,H", [(64, 1000, 512), (200, 3001, 264), (300, 33001, 264), (512, 70000, 64)])
+def test_a_factor_of_one(N, V, H):
+    """S / N * 2^-14 = 1: the products then take the kernels of ordinary calls where nothing else is asked of them.  A gradient may
+    be beyond FP16 here (16384 |x| for a label's word, |x| > 4): infinite then, with its sign."""
+    x, W, y = make(N, V, H, N + V, scale=0.5)
+    got = call(x, W, y, 16384.0 * N)
+    X, M, at = torch.from_numpy(x).cuda().double(), torch.from_numpy(W).cuda().double(), torch.from_numpy(y).cuda().long()
+    d = torch.softmax(X @ M.T, 1)
+    d[torch.arange(N, device="cuda"), at] -= 1.0
+    for name, ref in (("dx", 16384.0 * (d @ M)), ("dW", 16384.0 * (d.T @ X))):
+        over = got[name].isinf()
+        assert bool((ref[over].abs() >= 65504.0 * (1 - 4 * H16)).all()) and bool((ref[over].sign() == got[name][over].sign()).all())
+        got[name] = torch.where(over, ref, got[name].double())
+    check(x, W, y, 16384.0 * N, got)
