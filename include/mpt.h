@@ -518,11 +518,11 @@ void mpt_lstm_destroy(mpt_lstm_ctx *ctx);
  * workspace: mpt_layernorm_workspace_bytes, 16-byte aligned, owned by the caller and in use until the call's
  * stream work has completed (calls that may overlap need one each).  Results are run-to-run identical.
  * Fastest where all rows and the parameters are 16-byte aligned (base pointers, and pitches that are multiples of 8); rows
- * that are not are shifted on the way (about 1.6 times as long); rows of more than 16384 features forward, 12288
- * backward, are read more than once (by kernels that keep nothing of a row on chip).  cols from 1 to 2^30, rows from
- * 0 to 2^30 (MPT_ERR_SHAPE otherwise).  Outputs must not overlap inputs (the same pointer is refused).  rows == 0:
- * forward does nothing, backward writes zero dgamma and dbeta, and what holds rows may be null.  The stream must belong to the current device (the
- * launch fails otherwise: MPT_ERR_CUDA).  Bytes moved per element: 4 forward, 6 backward. */
+ * that are not are shifted on the way (about 1.6 times as long forward, twice backward); rows of more than 16384 features
+ * forward, 12288 backward, are read more than once (by kernels that keep nothing of a row on chip).  cols from 1 to 2^30, rows
+ * from 0 to 2^30 (MPT_ERR_SHAPE otherwise).  Outputs must not overlap inputs (the same pointer is refused).  rows == 0: forward
+ * does nothing, backward writes zero dgamma and dbeta, and what holds rows may be null.  The stream must belong to the current
+ * device (the launch fails otherwise: MPT_ERR_CUDA).  Bytes moved per element: 4 forward, 6 backward. */
 int mpt_layernorm_forward(int rows, int cols, const uint16_t *x_dev, int ldx, const uint16_t *gamma16_dev,
                           const uint16_t *beta16_dev, float eps, uint16_t *y_dev, int ldy, float *mean_dev, float *rstd_dev,
                           uint32_t *status_dev, void *cuda_stream);
@@ -543,22 +543,25 @@ int mpt_softmax_ce(const uint16_t *z_dev, int ldz, const int32_t *labels_dev, in
                    uint16_t *dz_dev, int lddz, float *row_loss_dev, float *loss_dev,
                    uint32_t *bad_labels_dev, uint32_t *status_dev, void *cuda_stream);
 
-/* Linear layer over a large vocabulary and the softmax cross-entropy of its outputs in one call, without a logits
- * matrix (sections 3.2, 3.3; the paper's language model, section 4.5, has 793K words and samples them instead).
+/* Linear layer over a large vocabulary and the softmax cross-entropy of its outputs in one call; the logits are not
+ * stored (sections 3.2, 3.3; the paper's language model, section 4.5, has 793K words and samples them instead).
  *   z[i,v]  = sum_k x[i,k] * W[v,k]                          FP32, never stored or rounded
  *   loss_i  = log sum_v exp(z[i,v]) - z[i,y_i]               row_loss_dev[i]; loss_dev = mean over the N rows
  *   d[i,v]  = softmax(z_i)[v] - [v = y_i]
  *   dx[i,:] = rn16(S/N * sum_v d[i,v] * W[v,:])              FP32 sums, S/N applied before the rounding
  *   dW[v,:] = rn16(S/N * sum_i d[i,v] * x[i,:])
- * The two gradients' products take d as FP16 scaled by 2^14 (rounded twice, each time by at most 2^-11 of the
- * value down to d = 2^-28, and kept down to 2^-38), so no d is lost to a small S/N.  Logits may be of any size (a class whose
- * weights make its logit smaller than the row's largest by some hundreds, however far, -inf included, has p = 0; where all of a
- * row's are -inf, or one is +inf, its loss and gradients are NaN).
+ * A logit is the sum of one tensor-core accumulator over all H features, which drops bits towards zero at each of its H / 16
+ * additions: it may be off by (H / 16 + 8) 2^-23 of the sum of its terms' absolute values, and the losses with it (ordinary
+ * rows of 12288 features: 4e-6).  The two gradients' products take d as FP16 scaled by 2^14 (rounded twice, each time by at most
+ * 2^-11 of the value down to d = 2^-28, and kept down to 2^-38), so no d is lost to a small S/N.  Logits may be of any size (a
+ * class whose weights make its logit smaller than the row's largest by some hundreds, however far, -inf included, has p = 0,
+ * though infinite weights are 0 * inf = NaN in dx; where all of a row's logits are -inf, or one is +inf, its loss and gradients are
+ * NaN).
  * x: FP16 [N, H], W: FP16 [V, H], dx like x, dW like W, row-major with pitches in elements; labels: int32 [N]
  * on the device.  A label outside [0, V) contributes neither loss nor gradient, whatever its row of x holds (its
  * row of dx is zero where W is finite; the mean still divides by N).  dx_dev and dW_dev may each be null (not wanted;
- * with both null only the losses are computed and S is ignored).  Gradients are overwritten, not accumulated into.  N == 0: loss 0, dW
- * zero, and what holds rows may be null.
+ * with both null only the losses are computed and S is ignored).  Gradients are overwritten, not accumulated into.  N == 0:
+ * loss 0, dW zero, and what holds rows may be null.
  * bad_labels_dev (may be null): receives the number of labels outside [0, V).  nonfinite_flag_dev (may be null):
  * OR-ed with 1 if any dW is inf or NaN (section 3.2).  status_dev (may be null): one uint32 the caller has zeroed,
  * receives a time-out code if a bounded wait of a product kernel runs out (results are then invalid).
@@ -568,7 +571,8 @@ int mpt_softmax_ce(const uint16_t *z_dev, int ldz, const int32_t *labels_dev, in
  * dx_dev, dW_dev will be given), owned by the caller and in use until the call's stream work has completed: calls
  * that may overlap, captured graphs among them, need one each.  The rows are worked on row_block at a time (a
  * multiple of 256, at most 65536; 0: the library's choice of 4096), which bounds the workspace: about 2 * row_block * V bytes of FP16
- * exponentials and 2 * row_block * H of x, and with more than one block 4 * V * H bytes in which dW is summed in FP32.
+ * exponentials and 2 * row_block * H of x, and with more than one block 4 * V * H bytes in which dW is summed in FP32 (a pass over
+ * those sums for each block: 4096 x 32000 x 12288 takes 7.6 ms in one block, 9.3 in two, 27 in eight).
  * Results are run-to-run identical.  Asynchronous on the stream, which must belong to the current device. */
 #define MPT_LINEAR_CE_MAX_V (1 << 24)
 int mpt_linear_ce_workspace_bytes(int N, int V, int H, int want_dx, int want_dW, int row_block, size_t *bytes_out);

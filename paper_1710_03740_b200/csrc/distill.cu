@@ -13,7 +13,7 @@
 // and about 6 instructions a logit (4096 x 32000 102 us = 5.1 TB/s, 2001 x 20011 43 us, 4096 x 32001 without a pitch, where
 // every row lies differently to 16-byte boundaries, 117 us).
 //   longer: k_distill_stream.  A row passes through shared memory twice, the second time from L2 (first reads are marked to
-// stay, second reads and the gradient to leave first), and its exponentials are taken twice (512 x 793471 364 us); where there
+// stay, second reads and the gradient to leave first), and its exponentials are taken twice (512 x 793471 364 to 389 us); where there
 // are few rows, or where that evens out the last round, the CTAs of a cluster share it and exchange the pairs through
 // distributed shared memory.
 #include <math.h>

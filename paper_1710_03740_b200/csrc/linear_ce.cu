@@ -1,6 +1,6 @@
 // Linear layer over a large vocabulary fused with the softmax cross-entropy of its outputs (paper sections 3.2,
-// 3.3: FP16 operands, FP32 sums and softmax arithmetic, gradient multiplied by S / N before it is rounded), without
-// a logits matrix and without rounding the logits:
+// 3.3: FP16 operands, FP32 sums and softmax arithmetic, gradient multiplied by S / N before it is rounded).  The logits are
+// neither rounded nor stored; for the gradients a block of rows keeps FP16 exponentials of them:
 //
 //   z = x . W^T in FP32 ;  loss_i = log sum_v exp(z_iv) - z_i,y(i)
 //   dx = rn16(S / N * sum_v (p_iv - [v = y(i)]) W_v) ;  dW_v = rn16(S / N * sum_i (p_iv - [v = y(i)]) x_i)
@@ -15,7 +15,7 @@
 //      in the epilogue (up to 128 rows: dW by k_ce_dw)
 // Keeping the exponentials costs 2 bytes a logit of a block and step 3 (4 bytes a logit through HBM: 143/H of the
 // products' time), computing them a second time would cost a fourth product (1/3).  FP16 keeps them, and p, to
-// 2^-12 of the value whatever S and N: the scale 2^14 leaves 2^-38 of a group's largest term (resp. of 1) above
+// 2^-11 of the value each (together 2.8e-4 on average, which is what dx and dW are off) whatever S and N: the scale 2^14 leaves 2^-38 of a group's largest term (resp. of 1) above
 // zero, where p * S / N in FP16 would lose p below 2^-24 N / S.  Over several row blocks dW is summed in FP32.
 // Measured: 4096 x 32000 x 12288 7.4-8.5 ms (1.13-1.3 PFLOP/s, under the power cap), 1024 x 793471 x 1024 5.4-6.3 ms,
 // losses alone 2500 x 50001 x 2048 0.41 ms (1.25 PFLOP/s), 64 x 1000 x 512 20 us.
@@ -236,11 +236,14 @@ __global__ void __launch_bounds__(256) k_ce_finish(uint16_t *__restrict__ e16, i
 }
 
 // dW of few rows, d^T x with a contraction over at most 128 rows: writing dW is what takes time, and the tcgen05 kernels, whose
-// epilogues reach 1.5 to 2.2 TB/s, are bound by that (whole calls of 3 rows, 136611 x 2304: 643 us, with this kernel 390; 64 rows,
-// 50000 x 2048: 229 and 187; 128 rows, 50000 x 1024: 156 and 154).  Here the
-// sums are in registers as they are made (warp-wide mma with FP32 sums: at 16 to 128 terms a sum it costs less than the
-// stores), pass through shared memory and leave in 16-byte stores.  A CTA keeps x for 128 features and goes through the words
-// 128 at a time, the next 128 words' d on the way meanwhile.
+// epilogues reach 1.5 to 2.2 TB/s, are bound by that.  Here the sums are in registers as they are made (warp-wide mma with FP32
+// sums), pass through shared memory and leave in 16-byte stores: 4.9 TB/s for 3 rows of 136611 x 2304, where the stores are the
+// bound, 1.8 TB/s for 96 rows, where mma.sync and the waits for d are (tensor pipe 46 %, one buffer of d).
+// Whole calls in us, the product kernel and this one: 3 rows, 136611 x 2304 643 and 390; 64 rows, 50000 x 2048 229 and 187; 82 rows,
+// 8491 x 9776 225 and 200; 128 rows, 32000 x 4096 294 and 276, 136611 x 2304 661 and 604, 50000 x 1024 156 and 156.  For few features
+// and 65 to 128 rows the product kernel would be the faster: 20000 x 512 63 and 65, 793471 x 1024 1435 and 1605.
+// A CTA keeps x for 128 features and goes through the words 128 at a time, up to 64 rows the next 128 words' d on the way
+// meanwhile.
 constexpr int kDwRows = 128, kDwTile = 128, kDwPitch = kDwTile + 8;      // pitch: 8 rows of a matrix load lie in different banks
 __device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr)
 {
